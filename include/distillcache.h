@@ -249,6 +249,25 @@ dc_status dc_evict(dc_cache* h, int budget);
  * q and out as in dc_decode_step. */
 dc_status dc_full_decode(dc_cache* h, const void* q, float* out);
 
+/* Attention of a tree of drafted tokens over the cache (speculative decoding):
+ * every drafted token of a sequence attends to all cached tokens of its rows, to
+ * its ancestors in the tree and to itself. Nothing is appended, scored or evicted:
+ * the tokens that the model accepts are appended afterwards (dc_append, dc_step).
+ *   q:       bf16 [layers][batch][nodes][q_heads][head_dim];
+ *   k_draft, v_draft: bf16 [layers][batch][kv_heads][nodes][head_dim];
+ *   parents: int32 [batch][nodes]: the node that node i follows, -1 for one that
+ *            follows the cached tokens directly. Parents come before their children:
+ *            a node whose parent is below -1 or not below its own index is unused (so
+ *            smaller trees share a batch), and so is a node that follows an unused one;
+ *   out:     bf16 [layers][batch][nodes][q_heads][head_dim]; 0 for unused nodes.
+ * bf16 output (the type of the product that takes it): the attention weights enter
+ * the second product as bf16. nodes <= 128; one node is a single token; the cache may
+ * be empty. Rows of different lengths (dc_set_row_budgets) are taken. A key or value
+ * that a node does not see leaves its output alone, whatever it holds. Launches count
+ * as DC_PHASE_FULL. */
+dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const void* v_draft,
+                         const int* parents, int nodes, void* out);
+
 /* Current tokens per row (every row holds the same number) and tokens seen. */
 dc_status dc_get_length(dc_cache* h, int* n, long long* seen);
 
@@ -283,7 +302,7 @@ typedef enum {
   DC_PHASE_SCORE = 3,   /* attention output, features and policy scores (split) */
   DC_PHASE_COMBINE = 4, /* per-split output merge (split) */
   DC_PHASE_EVICT = 5,   /* top-B select and compaction */
-  DC_PHASE_FULL = 6,    /* full-cache comparator */
+  DC_PHASE_FULL = 6,    /* full-cache comparator, drafted trees */
   DC_PHASE_COUNT = 7
 } dc_phase;
 
@@ -332,6 +351,85 @@ dc_status dc_attend_noalloc(const void* q, const void* k, const void* v, int row
 
 /* Message of the last failed dc_attend_noalloc call on this host thread. */
 const char* dc_noalloc_last_error(void);
+
+/* ---------------------------------------------------------------------------
+ * Before the cache: queries and keys, and a prompt's own attention. Handle-free
+ * (a plan holds lengths only), asynchronous on `stream` (a cudaStream_t, NULL for the
+ * default stream).
+ * ------------------------------------------------------------------------- */
+
+typedef enum { DC_BF16 = 0, DC_FP16 = 1 } dc_dtype;
+
+/* Tensors of dc_norm_rotate; strides in elements, the innermost one is 1. */
+typedef struct {
+  long long tokens;
+  int q_heads, kv_heads;     /* either may be 0 */
+  int head_dim;              /* a multiple of 8 in [16, 256] */
+  int rotary_dim;            /* the first dims, which are rotated: a multiple of 16 */
+  int dtype;                 /* dc_dtype of q, k and their outputs */
+  int norm;                  /* 1: root-mean-square norm of each head before the rotation */
+  int interleaved;           /* 0: dim j turns with dim j + rotary_dim / 2; 1: dim 2 j with 2 j + 1 */
+  float eps;
+  const int* positions;      /* [tokens], any value */
+  const float* inv_freq;     /* [rotary_dim / 2]: pair j turns by position * inv_freq[j] */
+  const float* q_weight;     /* [head_dim] gains of the norm, NULL: 1 */
+  const float* k_weight;
+  const void *q, *k;         /* [tokens][heads][head_dim] */
+  void *q_out, *k_out;       /* may be q and k themselves (same strides) */
+  long long q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  long long q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+} dc_rotate_args;
+
+/* Norms of queries and keys for each head and the position rotation in one pass:
+ * y = x / sqrt(mean(x^2) + eps) * w (or y = x), pairs (a, b) of y's first rotary_dim dims
+ * become (a cos t - b sin t, b cos t + a sin t) with t = position * inv_freq[j]. In 32
+ * bits, rounded once; the angle is reduced exactly, so that large positions lose
+ * nothing. Every head must start on 16 bytes (strides multiples of 8). Outputs must not
+ * overlap inputs other than by being them. DC_ERR_INVALID_ARG (message in
+ * dc_rotate_last_error()) for anything else. */
+dc_status dc_norm_rotate(const dc_rotate_args* args, void* stream);
+
+/* Message of the last failed dc_norm_rotate call on this host thread. */
+const char* dc_rotate_last_error(void);
+
+/* What dc_prompt_attend does for packed sequences of given lengths: the division of
+ * the work, kept on the device. Never written after creation: calls with one plan
+ * may overlap on any streams of its device, and be captured. */
+typedef struct dc_prompt_plan dc_prompt_plan;
+
+/* Plans the attention of n packed sequences (host arrays): sequence s has q_lens[s]
+ * queries, its last ones, over k_lens[s] keys (NULL: q_lens). causal: query i of a
+ * sequence sees its keys 0 .. i + k_len - q_len, so a prompt has equal lengths, a
+ * chunk or a chat turn has more keys, a single token one query; a query with no key
+ * (k_len < q_len) gets output 0. causal 0: every query sees every key. head_dim 64 or
+ * 128, q_heads = kv_heads times 1 to 128, lengths >= 0. Allocates on the current
+ * device and synchronises. */
+dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int q_heads, int kv_heads,
+                                int head_dim, int causal, dc_prompt_plan** out);
+
+/* Frees the plan (its calls must have finished). NULL is a no-op. */
+dc_status dc_prompt_plan_destroy(dc_prompt_plan* p);
+
+/* Tensors of dc_prompt_attend; strides in elements, the innermost one is 1. */
+typedef struct {
+  int dtype;             /* dc_dtype of q, k, v and out */
+  float scale;           /* > 0; 1 / sqrt(head_dim) as a rule */
+  const void* q;         /* [sum of q_lens][q_heads][head_dim] */
+  const void *k, *v;     /* [sum of k_lens][kv_heads][head_dim] */
+  long long q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  void* out;             /* [sum of q_lens][q_heads][head_dim], dense */
+  float* lse;            /* [sum of q_lens][q_heads] log of the softmax denominator, or NULL */
+} dc_prompt_args;
+
+/* Softmax attention as planned; query head j uses KV head j / (q_heads / kv_heads).
+ * Sums and statistics in 32 bits, the weights rounded to `dtype` for the second
+ * product, one rounding of the output. A key or value that a query does not see
+ * leaves its output alone, whatever it holds; lse is -infinity where a query sees
+ * no key. 16-byte aligned tensors, strides multiples of 8. */
+dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, void* stream);
+
+/* Message of the last failed dc_prompt_* call on this host thread. */
+const char* dc_prompt_last_error(void);
 
 /* Self-test of the bounded waits every kernel relies on (a wait that cannot be
  * satisfied gives up after its time limit, records where and lets the kernel

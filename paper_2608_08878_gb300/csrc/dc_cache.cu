@@ -16,6 +16,7 @@
 #include "dc_common.cuh"
 #include "dc_fused.h"
 #include "dc_kernels.h"
+#include "dc_prompt.h"
 
 namespace {
 
@@ -1007,6 +1008,50 @@ dc_status dc_full_decode(dc_cache* h, const void* q, float* out) {
   }
   if (!ok) return fail(h, DC_ERR_INVALID_ARG, "unsupported head_dim / group");
   return launch_error(h, "full decode");
+}
+
+dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const void* v_draft, const int* parents,
+                         int nodes, void* out) {
+  DC_CHECK_HANDLE(h);
+  if (h->graph) return fail(h, DC_ERR_STATE, "graph mode: only dc_step and its host forms until dc_set_graph_mode(h, 0)");
+  if (nodes < 0 || nodes > dc::kMaxNodes) return fail(h, DC_ERR_INVALID_ARG, "a tree has at most 128 nodes");
+  if (nodes == 0) return DC_OK;
+  if (!q || !k_draft || !v_draft || !parents || !out) return fail(h, DC_ERR_INVALID_ARG, "NULL pointer");
+  if (((uintptr_t)q | (uintptr_t)k_draft | (uintptr_t)v_draft | (uintptr_t)out) & 15)
+    return fail(h, DC_ERR_INVALID_ARG, "q, k_draft, v_draft and out must be 16-byte aligned");
+  if ((uintptr_t)parents & 3) return fail(h, DC_ERR_INVALID_ARG, "parents must be 4-byte aligned");
+  const dc::Dev& p = h->dev;
+  dc::AttnArgs a{};
+  a.q = (const uint16_t*)q;
+  a.out = (uint16_t*)out;
+  a.q_h = a.o_h = p.d;
+  a.q_t = a.o_t = (long long)p.qh * p.d;
+  a.q_lb = a.o_lb = (long long)nodes * p.qh * p.d;
+  a.k = (const uint16_t*)p.K;
+  a.v = (const uint16_t*)p.V;
+  a.k_t = a.v_t = p.d;
+  a.k_y = a.v_y = (long long)p.stride * p.d;
+  a.kd = (const uint16_t*)k_draft;
+  a.vd = (const uint16_t*)v_draft;
+  a.G = p.G;
+  a.kvh = p.kvh;
+  a.scale = (float)(1.0 / std::sqrt((double)p.d));
+  a.c = p.c;
+  a.n = h->n;
+  a.nodes = nodes;
+  a.batch = p.batch;
+  a.rows = p.R;
+  a.rowlen = p.rowlen;
+  a.parents = parents;
+  a.status = p.status;
+  a.dbg = p.dbg;
+  cudaError_t e;
+  {
+    Phase ph(h, DC_PHASE_FULL, 1);
+    e = dc::launch_tree(a, p.d, h->num_sms, h->stream);
+  }
+  if (e != cudaSuccess) return cuda_fail(h, e, "tree attention");
+  return DC_OK;
 }
 
 dc_status dc_set_row_budgets(dc_cache* h, const int* budgets, int n) {

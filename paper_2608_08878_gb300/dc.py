@@ -35,7 +35,8 @@ EXPORTS = ["dc_config_default", "dc_cache_create", "dc_cache_destroy", "dc_polic
            "dc_noalloc_last_error", "dc_pl_log_partition", "dc_gumbel_top_b", "dc_train_last_error",
            "dc_set_row_budgets", "dc_get_row_lengths", "dc_wait_selftest", "dc_selftest_last_error",
            "dc_set_graph_mode", "dc_debug_fail_alloc", "dc_debug_checks", "dc_debug_bounds_selftest",
-           "dc_debug_corrupt_guard", "dc_debug_schedule"]
+           "dc_debug_corrupt_guard", "dc_debug_schedule", "dc_tree_attend", "dc_norm_rotate", "dc_rotate_last_error",
+           "dc_prompt_plan_create", "dc_prompt_plan_destroy", "dc_prompt_attend", "dc_prompt_last_error"]
 PHASES = ["append", "attend", "stats", "score", "combine", "evict", "full"]
 
 
@@ -46,6 +47,24 @@ class dc_config(C.Structure):
                 ("stream", C.c_void_p), ("tail_split", C.c_int), ("scorer", C.c_int),
                 ("n_sinks", C.c_int), ("budget_ratio", C.c_float), ("budget_min", C.c_int),
                 ("budget_basis", C.c_int), ("global_tokens", C.c_int)]
+
+
+class dc_rotate_args(C.Structure):
+    _fields_ = [("tokens", C.c_longlong), ("q_heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("rotary_dim", C.c_int), ("dtype", C.c_int), ("norm", C.c_int), ("interleaved", C.c_int),
+                ("eps", C.c_float), ("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("q", C.c_void_p), ("k", C.c_void_p), ("q_out", C.c_void_p),
+                ("k_out", C.c_void_p), ("q_token_stride", C.c_longlong), ("q_head_stride", C.c_longlong),
+                ("k_token_stride", C.c_longlong), ("k_head_stride", C.c_longlong),
+                ("q_out_token_stride", C.c_longlong), ("q_out_head_stride", C.c_longlong),
+                ("k_out_token_stride", C.c_longlong), ("k_out_head_stride", C.c_longlong)]
+
+
+class dc_prompt_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("scale", C.c_float), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_token_stride", C.c_longlong), ("q_head_stride", C.c_longlong), ("k_token_stride", C.c_longlong),
+                ("k_head_stride", C.c_longlong), ("v_token_stride", C.c_longlong), ("v_head_stride", C.c_longlong),
+                ("out", C.c_void_p), ("lse", C.c_void_p)]
 
 
 class DCError(RuntimeError):
@@ -95,6 +114,15 @@ def lib():
             L.dc_gumbel_top_b.argtypes = [P, P, I, I, I, C.c_float, P, P, P, P]
             L.dc_train_last_error.argtypes = []
             L.dc_train_last_error.restype = C.c_char_p
+            L.dc_tree_attend.argtypes = [P, P, P, P, P, I, P]
+            L.dc_norm_rotate.argtypes = [C.POINTER(dc_rotate_args), P]
+            L.dc_rotate_last_error.argtypes = []
+            L.dc_rotate_last_error.restype = C.c_char_p
+            L.dc_prompt_plan_create.argtypes = [P, P, I, I, I, I, I, C.POINTER(P)]
+            L.dc_prompt_plan_destroy.argtypes = [P]
+            L.dc_prompt_attend.argtypes = [P, C.POINTER(dc_prompt_args), P]
+            L.dc_prompt_last_error.argtypes = []
+            L.dc_prompt_last_error.restype = C.c_char_p
             L.dc_wait_selftest.argtypes = [C.c_ulonglong, P, P]
             L.dc_debug_fail_alloc.argtypes = [C.c_longlong]
             L.dc_debug_checks.argtypes = []
@@ -115,7 +143,8 @@ def lib():
             L.dc_profile_read.argtypes = [P, P, P]
             for name in EXPORTS:
                 if name not in ("dc_policy_blob_len", "dc_last_error", "dc_phase_name", "dc_noalloc_last_error",
-                                "dc_train_last_error", "dc_selftest_last_error"):
+                                "dc_train_last_error", "dc_selftest_last_error", "dc_rotate_last_error",
+                                "dc_prompt_last_error"):
                     getattr(L, name).restype = I
             _lib = L
     return _lib
@@ -291,6 +320,177 @@ def _arg(t, name: str, dtype, numel: int, cuda: bool = True, device: int | None 
     return int(t.data_ptr())
 
 
+def _heads(t, name: str, heads: int | None, dim: int | None, dtype, device: int):
+    """(address, token stride, head stride) of a [tokens][heads][head_dim] tensor, which may be a view (of a
+    fused projection's output, or head by head), after checking what the library assumes of it."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} must be a [tokens][heads][head_dim] tensor")
+    if not t.is_cuda or t.device.index != device:
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected cuda:{device}")
+    if t.dtype != dtype:
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} must be {dtype}, got {t.dtype}")
+    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}, expected (tokens, {heads}, {dim})")
+    st, sh, sd = t.stride()
+    T, H, D = t.shape
+    # (the stride of a dimension of one says nothing)
+    st, sh = (st if T > 1 else H * D), (sh if H > 1 else D)
+    if sd != 1 or st % 8 or sh % 8 or st < 0 or sh < 0 or t.data_ptr() % 16:
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} must start every head on 16 bytes (strides {tuple(t.stride())})")
+    return t.data_ptr(), st, sh
+
+
+def _fresh(t, name: str, shape):
+    """Checks that the output tensor t, if given, has this shape and no two places for one value."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape):
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    dims = sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1)
+    if any(s < s0 * n0 for (s0, n0), (s, _) in zip(dims, dims[1:])) or (dims and dims[0][0] < 1):
+        raise DCError(DC_ERR_INVALID_ARG, f"{name}'s elements overlap (strides {tuple(t.stride())})")
+
+
+class _on:
+    """The stream that a handle-free call runs on, made current, so that what the call allocates belongs to it;
+    tensors made on another stream are told that this one uses them."""
+
+    def __init__(self, device, stream, *tensors):
+        import torch
+        if stream is not None and stream.device != device:
+            raise DCError(DC_ERR_INVALID_ARG, f"stream is on {stream.device}, the tensors on {device}")
+        self.stream = stream or torch.cuda.current_stream(device)
+        if stream is not None and stream != torch.cuda.current_stream(device):
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+        self.ctx = torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        self.ctx.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *a):
+        self.ctx.__exit__(*a)
+
+
+def _dtype16(t, name: str) -> int:
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.bfloat16, torch.float16):
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} must be a bfloat16 or float16 tensor")
+    if not t.is_cuda:
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} must be a CUDA tensor")
+    return 0 if t.dtype == torch.bfloat16 else 1
+
+
+def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps: float = 1e-6, norm: bool = True,
+                interleaved: bool = False, q_out=None, k_out=None, stream=None):
+    """Norms of queries and keys for each head and the position rotation in one pass.
+
+    q [tokens][q_heads][d], k [tokens][kv_heads][d]: bf16 or fp16 CUDA tensors, also views (of a fused
+    projection's output); positions int32 [tokens]; inv_freq fp32 [r / 2] for the first r dims, which are
+    rotated (pair j by position * inv_freq[j]; dims (j, j + r / 2), or (2j, 2j + 1) if interleaved);
+    q_weight, k_weight fp32 [d]: gains of the norm (None: 1); norm=False: rotation only.
+    q_out, k_out: where the results go, of q's and k's shape (views too, so that keys can go straight into
+    `append`'s [kv_heads][tokens][d]; q and k themselves: in place). Returns (q_out, k_out)."""
+    import torch
+    a = dc_rotate_args()
+    a.dtype = _dtype16(q, "q")
+    dev = q.device.index
+    a.q, a.q_token_stride, a.q_head_stride = _heads(q, "q", None, None, q.dtype, dev)
+    T, a.q_heads, d = q.shape
+    a.k, a.k_token_stride, a.k_head_stride = _heads(k, "k", None, d, q.dtype, dev)
+    if k.shape[0] != T:
+        raise DCError(DC_ERR_INVALID_ARG, f"q has {T} tokens, k {k.shape[0]}")
+    a.tokens, a.kv_heads, a.head_dim = T, k.shape[1], d
+    a.norm, a.interleaved, a.eps = int(bool(norm)), int(bool(interleaved)), eps
+    a.positions = _arg(positions, "positions", torch.int32, T, device=dev)
+    if not isinstance(inv_freq, torch.Tensor):
+        raise DCError(DC_ERR_INVALID_ARG, "inv_freq must be a torch tensor")
+    a.rotary_dim = 2 * inv_freq.numel()
+    a.inv_freq = _arg(inv_freq, "inv_freq", torch.float32, inv_freq.numel(), device=dev)
+    a.q_weight = None if q_weight is None else _arg(q_weight, "q_weight", torch.float32, d, device=dev)
+    a.k_weight = None if k_weight is None else _arg(k_weight, "k_weight", torch.float32, d, device=dev)
+    outs = {"q_out": q_out, "k_out": k_out}
+    for name, like in (("q_out", q), ("k_out", k)):
+        if outs[name] is not None:
+            _heads(outs[name], name, like.shape[1], d, q.dtype, dev)
+            _fresh(outs[name], name, like.shape)
+    with torch.cuda.device(dev), _on(q.device, stream, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out) as s:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        a.q_out, a.q_out_token_stride, a.q_out_head_stride = _heads(q_out, "q_out", a.q_heads, d, q.dtype, dev)
+        a.k_out, a.k_out_token_stride, a.k_out_head_stride = _heads(k_out, "k_out", a.kv_heads, d, q.dtype, dev)
+        st = lib().dc_norm_rotate(C.byref(a), s)
+    if st != DC_OK:
+        raise DCError(st, lib().dc_rotate_last_error().decode())
+    return q_out, k_out
+
+
+class PromptPlan:
+    """The division of the work of attention over packed sequences of given lengths (see
+    dc_prompt_plan_create), on the current CUDA device; one plan serves every layer of a forward pass."""
+
+    def __init__(self, q_lens, kv_heads: int, head_dim: int, *, q_heads: int | None = None, k_lens=None,
+                 causal: bool = True):
+        import torch
+        ql = np.ascontiguousarray(q_lens, dtype=np.int32).ravel()
+        kl = ql if k_lens is None else np.ascontiguousarray(k_lens, dtype=np.int32).ravel()
+        if kl.size != ql.size:
+            raise DCError(DC_ERR_INVALID_ARG, f"{ql.size} query lengths, {kl.size} key lengths")
+        self._p = None
+        self.kv_heads, self.head_dim, self.q_heads = kv_heads, head_dim, 4 * kv_heads if q_heads is None else q_heads
+        self.q_tokens, self.k_tokens = int(ql.sum(dtype=np.int64)), int(kl.sum(dtype=np.int64))
+        p = C.c_void_p()
+        st = lib().dc_prompt_plan_create(ql.ctypes.data_as(C.c_void_p), kl.ctypes.data_as(C.c_void_p), ql.size,
+                                         self.q_heads, kv_heads, head_dim, int(bool(causal)), C.byref(p))
+        if st != DC_OK:
+            raise DCError(st, lib().dc_prompt_last_error().decode())
+        self._p = p
+        self.device = torch.cuda.current_device()
+
+    def close(self) -> None:
+        if getattr(self, "_p", None):
+            lib().dc_prompt_plan_destroy(self._p)
+            self._p = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def attend(self, q, k, v, *, out=None, with_lse: bool = False, scale: float | None = None, stream=None):
+        """q [sum of q_lens][q_heads][d], k, v [sum of k_lens][kv_heads][d]: bf16 or fp16 CUDA tensors, also
+        views -> out [sum of q_lens][q_heads][d] of q's type; with_lse: (out, the log of each softmax's
+        denominator, fp32 [sum of q_lens][q_heads]). scale: 1 / sqrt(d) by default."""
+        import torch
+        if not self._p:
+            raise DCError(DC_ERR_INVALID_ARG, "the plan is closed")
+        a = dc_prompt_args()
+        a.dtype = _dtype16(q, "q")
+        d, dev = self.head_dim, self.device
+        a.q, a.q_token_stride, a.q_head_stride = _heads(q, "q", self.q_heads, d, q.dtype, dev)
+        a.k, a.k_token_stride, a.k_head_stride = _heads(k, "k", self.kv_heads, d, q.dtype, dev)
+        a.v, a.v_token_stride, a.v_head_stride = _heads(v, "v", self.kv_heads, d, q.dtype, dev)
+        if q.shape[0] != self.q_tokens or k.shape[0] != self.k_tokens or v.shape[0] != self.k_tokens:
+            raise DCError(DC_ERR_INVALID_ARG, f"q, k and v have {q.shape[0]}, {k.shape[0]} and {v.shape[0]} tokens, the plan "
+                          f"{self.q_tokens} and {self.k_tokens}")
+        a.scale = 1.0 / d ** 0.5 if scale is None else scale
+        if out is not None:
+            _fresh(out, "out", q.shape)
+            _arg(out, "out", q.dtype, q.numel(), device=dev)
+        with torch.cuda.device(dev), _on(q.device, stream, q, k, v, out) as s:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+            a.out, a.lse = _ptr(out), _ptr(lse)
+            st = lib().dc_prompt_attend(self._p, C.byref(a), s)
+        if st != DC_OK:
+            raise DCError(st, lib().dc_prompt_last_error().decode())
+        return (out, lse) if with_lse else out
+
+
 class DistillCache:
     """A budgeted KV cache of ``layers x batch x kv_heads`` rows on the current
     CUDA device, driven through the C ABI on one CUDA stream."""
@@ -435,6 +635,28 @@ class DistillCache:
         pq = _arg(q, "q", torch.bfloat16, nq, device=self.device)
         po = _arg(out, "out", torch.float32, nq, device=self.device)
         self._check(lib().dc_full_decode(self._h, pq, po))
+        return out
+
+    def tree_attend(self, q, k_draft, v_draft, parents, out=None):
+        """Attention of drafted trees over the cache, which stays as it is (see dc_tree_attend).
+
+        q bf16 [layers][batch][nodes][q_heads][d]; k_draft, v_draft bf16 [layers][batch][kv_heads][nodes][d];
+        parents int32 [batch][nodes] (the node that node i follows, -1: the cached tokens; below -1: unused)
+        -> out bf16 like q (0 for unused nodes)."""
+        import torch
+        if not isinstance(parents, torch.Tensor) or parents.dim() != 2 or parents.shape[0] != self.batch:
+            raise DCError(DC_ERR_INVALID_ARG, f"parents must be an int32 [{self.batch}][nodes] tensor")
+        T = int(parents.shape[1])
+        n = self.layers * self.batch * T * self.head_dim
+        pp = _arg(parents, "parents", torch.int32, self.batch * T, device=self.device)
+        pq = _arg(q, "q", torch.bfloat16, n * self.q_heads, device=self.device)
+        pk = _arg(k_draft, "k_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
+        pv = _arg(v_draft, "v_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
+        if out is None:
+            with torch.cuda.stream(self.stream):
+                out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        po = _arg(out, "out", torch.bfloat16, n * self.q_heads, device=self.device)
+        self._check(lib().dc_tree_attend(self._h, pq, pk, pv, pp, T, po))
         return out
 
     def set_row_budgets(self, budgets) -> None:
