@@ -393,8 +393,9 @@ dc_status dc_norm_rotate(const dc_rotate_args* args, void* stream);
 const char* dc_rotate_last_error(void);
 
 /* What dc_prompt_attend does for packed sequences of given lengths: the division of
- * the work, kept on the device. Never written after creation: calls with one plan
- * may overlap on any streams of its device, and be captured. */
+ * the work, kept on the device. Calls write nothing of it but the status word of a
+ * failed wait (dc_prompt_check): they may overlap on any streams of its device, with a
+ * workspace each, and be captured. */
 typedef struct dc_prompt_plan dc_prompt_plan;
 
 /* Plans the attention of n packed sequences (host arrays): sequence s has q_lens[s]
@@ -419,7 +420,13 @@ typedef struct {
   long long q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
   void* out;             /* [sum of q_lens][q_heads][head_dim], dense */
   float* lse;            /* [sum of q_lens][q_heads] log of the softmax denominator, or NULL */
+  void* workspace;       /* dc_prompt_workspace bytes, or NULL where that is 0 */
+  size_t workspace_bytes;
 } dc_prompt_args;
+
+/* Device memory that a call needs for the partial results of work that is split over
+ * long key sequences (0 where there is none); its contents need not be kept. */
+dc_status dc_prompt_workspace(const dc_prompt_plan* p, size_t* bytes);
 
 /* Softmax attention as planned; query head j uses KV head j / (q_heads / kv_heads).
  * Sums and statistics in 32 bits, the weights rounded to `dtype` for the second
@@ -427,6 +434,10 @@ typedef struct {
  * leaves its output alone, whatever it holds; lse is -infinity where a query sees
  * no key. 16-byte aligned tensors, strides multiples of 8. */
 dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, void* stream);
+
+/* Waits for the stream; DC_ERR_DEVICE if a kernel of the plan has reported an error
+ * (a wait inside it that ran out of time). */
+dc_status dc_prompt_check(const dc_prompt_plan* p, void* stream);
 
 /* Message of the last failed dc_prompt_* call on this host thread. */
 const char* dc_prompt_last_error(void);

@@ -33,9 +33,15 @@ struct AttnArgs {
   float scale, c;            // c = scale * log2(e)
   // prompts: the plan's items
   const struct AttnItem* items;
-  int n_items;
+  const int* first;          // CTA b takes items [first[b], first[b + 1])
+  const int2* merges;        // work split over keys: each group's first item and its parts
+  int n_items, n_merges;
+  // partial results: fp32 [slot][prows][D], and each row's m and l
+  float* part;
+  float2* part_ml;
+  int prows;
   // trees
-  int n, nodes, batch, rows, pairs;
+  int n, nodes, batch, rows, pairs, nsplit;
   const int* rowlen;         // each row's length, or null (n)
   const int* parents;        // [batch][nodes]
   unsigned* status;

@@ -98,6 +98,9 @@ struct dc_cache {
   dc::Step gstep{};
   unsigned gepoch = 0;
   int* gcount_dev = nullptr;
+  // partial results of dc_tree_attend's rows in parts (floats)
+  float* tree_part = nullptr;
+  size_t tree_len = 0;
   struct Alloc {
     void* base;    // what cudaMalloc returned (guard regions included in debug builds)
     size_t bytes;  // the buffer's own size
@@ -1045,11 +1048,28 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   a.parents = parents;
   a.status = p.status;
   a.dbg = p.dbg;
-  cudaError_t e;
-  {
-    Phase ph(h, DC_PHASE_FULL, 1);
-    e = dc::launch_tree(a, p.d, h->num_sms, h->stream);
+  const long long slots = dc::tree_plan(&a, p.d, h->num_sms);
+  if (slots) {
+    // the partial results of rows in parts: kept with the handle, and made larger when a call needs more
+    const size_t rows = (size_t)slots * a.prows;
+    if (rows * (p.d + 2) > h->tree_len) {
+      float* buf = nullptr;
+      cudaError_t ae = dalloc(h, &buf, rows * (p.d + 2) * sizeof(float));
+      if (ae != cudaSuccess) return alloc_fail(h, ae, "tree attention");
+      dfree(h, &h->tree_part);
+      h->tree_part = buf;
+      h->tree_len = rows * (p.d + 2);
+    }
+    a.part = h->tree_part;
+    a.part_ml = reinterpret_cast<float2*>(h->tree_part + rows * p.d);
   }
+  cudaError_t e;
+  const char* why = nullptr;
+  {
+    Phase ph(h, DC_PHASE_FULL, slots ? 2 : 1);
+    e = dc::launch_tree(a, p.d, p.stride, h->num_sms, h->stream, &why);
+  }
+  if (why) return fail(h, DC_ERR_INVALID_ARG, why);
   if (e != cudaSuccess) return cuda_fail(h, e, "tree attention");
   return DC_OK;
 }

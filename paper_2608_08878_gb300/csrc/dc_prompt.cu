@@ -2,34 +2,60 @@
 // dc_prompt_attend): the plan's work items and the C ABI.
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
+#include <functional>
+#include <memory>
 #include <new>
+#include <queue>
 #include <string>
 #include <vector>
 
 #include "../../include/distillcache.h"
+#include "dc_attend_kernel.cuh"
 #include "dc_prompt.h"
 
 namespace dc {
-namespace {
 
-// A block per item, a warp per query row.
-template <class T, int D>
-__global__ void __launch_bounds__(256) prompt_rows_kernel(AttnArgs a) {
-  const AttnItem it = a.items[blockIdx.x];
-  const int lane = threadIdx.x & 31, tpt = kAttRows / a.G;
-  const int t1 = min(it.tend, it.t0 + (it.alt ? 1 : 2) * tpt);
-  for (int r = threadIdx.x / 32; r < (t1 - it.t0) * a.G; r += 8) {
-    const int t = it.t0 + r / a.G, head = it.h * a.G + r % a.G, lim = att_limit(it, t);
-    float m, l, o[D / 32];
-    attend_row<T, D>(a, a.q + t * a.q_t + head * a.q_h, a.k + it.k0 * a.k_t + it.y * a.k_y,
-                     a.v + it.k0 * a.v_t + it.y * a.v_y, nullptr, nullptr, 0, lim, nullptr, m, l, o);
-    const float inv = lim > 0 ? 1.f / l : 0.f;
-    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + t * a.o_t + head * a.o_h) + lane * (D / 64);
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) to[e] = T::pack(o[2 * e] * inv, o[2 * e + 1] * inv);
-    if (a.lse && lane == 0) a.lse[(long long)t * a.kvh * a.G + head] = lim > 0 ? fmaf(m, a.scale, logf(l)) : -INFINITY;
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool att_map(CUtensorMap* m, bool bf16, const void* base, int rank, const long long* dims, const long long* strides,
+             const int* box) {
+  static const EncodeTiledFn encode = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+    return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiledFn>(fn) : nullptr;
+  }();
+  if (!encode) return false;
+  cuuint64_t d[5], st[4];
+  cuuint32_t b[5], one[5];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    b[i] = (cuuint32_t)box[i];
+    one[i] = 1;
+    if (i) st[i - 1] = dims[i] > 1 ? (cuuint64_t)strides[i - 1] * 2 : 16;
   }
+  return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+                const_cast<void*>(base), d, st, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+bool att_map_q(CUtensorMap* m, bool bf16, const AttnArgs& a, int D, long long tokens, long long lbs) {
+  const long long dims[5] = {D, a.G, a.kvh, tokens, lbs}, strides[4] = {a.q_h, a.G * a.q_h, a.q_t, a.q_lb};
+  const int box[5] = {64, a.G, 1, kAttRows / a.G, 1};
+  return att_map(m, bf16, a.q, 5, dims, strides, box);
+}
+
+bool att_map_kv(CUtensorMap* m, bool bf16, const void* base, int D, long long ys, long long y_stride, long long tokens,
+                long long t_stride) {
+  const long long dims[3] = {D, ys, tokens}, strides[2] = {y_stride, t_stride};
+  const int box[3] = {64, 1, kAttTok};
+  return att_map(m, bf16, base, 3, dims, strides, box);
+}
+
+namespace {
 
 thread_local std::string g_prompt_error;
 
@@ -53,17 +79,35 @@ struct dc_prompt_plan {
   int device = 0;
   int q_heads = 0, kv_heads = 0, head_dim = 0;
   long long q_tokens = 0, k_tokens = 0;
-  int n_items = 0;
-  dc::AttnItem* items = nullptr;  // device
+  int n_items = 0, n_merges = 0, n_slots = 0, prows = 0, grid = 0, num_sms = 0;
+  // device: one allocation, the status words first
+  unsigned* status = nullptr;     // [0] status, [8..15] the first failure
+  dc::AttnItem* items = nullptr;
+  int* first = nullptr;
+  int2* merges = nullptr;
+  size_t workspace() const { return (size_t)n_slots * prows * (head_dim + 2) * sizeof(float); }
 };
 
 namespace dc {
 namespace {
 
-std::vector<AttnItem> plan_items(const int* q_lens, const int* k_lens, int n, int kvh, int G, bool causal) {
+struct Division {
+  std::vector<AttnItem> items;  // CTA by CTA
+  std::vector<int> first;
+  std::vector<int2> merges;
+  int slots = 0, prows = 0;
+};
+
+// The time of an item in halves of a key tile's products with one tile of queries: two
+// products for each tile of queries and key tile (three halves where one tile of queries leaves
+// the tensor cores waiting for keys), and its start and end.
+double item_cost(const AttnItem& it) { return (it.j1 - it.j0) * (it.alt ? 1.5 : 2.0) + 3.0; }
+
+Division plan_items(const int* q_lens, const int* k_lens, int n, int kvh, int G, bool causal, int num_sms) {
   const int tpt = kAttRows / G;
-  std::vector<AttnItem> items;
+  std::vector<AttnItem> whole;
   long long q0 = 0, k0 = 0;
+  double total = 0;
   for (int s = 0; s < n; ++s) {
     const int ql = q_lens[s], kl = k_lens[s];
     for (int t = 0; t < ql; t += 2 * tpt)
@@ -74,20 +118,60 @@ std::vector<AttnItem> plan_items(const int* q_lens, const int* k_lens, int n, in
         it.tend = (int)(q0 + ql);
         it.k0 = (int)k0;
         it.klen = kl;
-        it.off = causal ? kl - ql + 1 - (int)q0 : kSeesAll;
-        const int last = std::min(it.tend, it.t0 + 2 * tpt) - 1;
-        it.j0 = 0;
-        it.j1 = (att_limit(it, last) + kAttTok - 1) / kAttTok;
+        it.off = causal ? (int)(kl - ql + 1 - q0) : kSeesAll;
+        it.j1 = (att_limit(it, std::min(it.tend, it.t0 + 2 * tpt) - 1) + kAttTok - 1) / kAttTok;
         it.slot = -1;
         it.alt = it.tend - it.t0 <= tpt;
-        items.push_back(it);
+        whole.push_back(it);
+        total += item_cost(it);
       }
     q0 += ql;
     k0 += kl;
   }
-  // the longest first
-  std::stable_sort(items.begin(), items.end(), [](const AttnItem& a, const AttnItem& b) { return a.j1 - a.j0 > b.j1 - b.j0; });
-  return items;
+  // Items longer than an SM's share are cut into parts of about that size (8 units at least:
+  // a part's partial results cost about as much), whose results a second kernel joins.
+  Division d;
+  const double share = std::max(8.0, total / num_sms);
+  std::vector<AttnItem> items;
+  std::vector<int> parts_of;  // of the item that starts a group, else 0
+  for (const AttnItem& it : whole) {
+    const int tiles = it.j1 - it.j0;
+    const int parts = std::max(1, std::min(tiles, (int)std::ceil((item_cost(it) - 3.0) / share)));
+    for (int p = 0; p < parts; ++p) {
+      AttnItem x = it;
+      x.j0 = it.j0 + (int)((long long)tiles * p / parts);
+      x.j1 = it.j0 + (int)((long long)tiles * (p + 1) / parts);
+      if (parts > 1) x.slot = d.slots++;
+      items.push_back(x);
+      parts_of.push_back(parts > 1 && p == 0 ? parts : 0);
+    }
+    if (parts > 1) d.prows = std::max(d.prows, it.alt ? (it.tend - it.t0) * G : 256);
+  }
+  // the longest first, each to the CTA with the least to do (few items: one each)
+  std::vector<int> order(items.size());
+  for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return item_cost(items[a]) > item_cost(items[b]); });
+  const int grid = (int)std::min<size_t>(items.size(), (size_t)num_sms);
+  std::vector<std::vector<int>> of(grid);
+  using Load = std::pair<double, int>;
+  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+  for (int b = 0; b < grid; ++b) least.push({0.0, b});
+  for (int i : order) {
+    Load x = least.top();
+    least.pop();
+    of[x.second].push_back(i);
+    x.first += item_cost(items[i]);
+    least.push(x);
+  }
+  for (int b = 0; b < grid; ++b) {
+    d.first.push_back((int)d.items.size());
+    for (int i : of[b]) {
+      if (parts_of[i]) d.merges.push_back(make_int2((int)d.items.size(), parts_of[i]));
+      d.items.push_back(items[i]);
+    }
+  }
+  d.first.push_back((int)d.items.size());
+  return d;
 }
 
 }  // namespace
@@ -116,33 +200,48 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
     kt += k_lens[s];
   }
   if (qt > (1 << 29) || kt > (1 << 29)) return prompt_fail(DC_ERR_INVALID_ARG, "at most 2^29 packed tokens");
-  int dev = 0;
+  int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return prompt_cuda(e, "cudaGetDevice");
-  const auto items = dc::plan_items(q_lens, k_lens, n, kv_heads, q_heads / kv_heads, causal != 0);
-  dc::AttnItem* d = nullptr;
-  if (!items.empty()) {
-    e = cudaMalloc(&d, items.size() * sizeof(dc::AttnItem));
-    if (e != cudaSuccess) {
-      cudaGetLastError();
-      return prompt_cuda(e, "plan allocation");
-    }
-    e = cudaMemcpy(d, items.data(), items.size() * sizeof(dc::AttnItem), cudaMemcpyHostToDevice);
-    if (e != cudaSuccess) {
-      cudaFree(d);
-      return prompt_cuda(e, "plan upload");
-    }
+  const dc::Division v = dc::plan_items(q_lens, k_lens, n, kv_heads, q_heads / kv_heads, causal != 0, sms);
+  // one block on the device: status words, items, each CTA's first item, merges
+  auto up = [](size_t x) { return (x + 15) / 16 * 16; };
+  const size_t at_items = 64, at_first = up(at_items + v.items.size() * sizeof(dc::AttnItem)),
+               at_merges = up(at_first + v.first.size() * sizeof(int)), bytes = up(at_merges + v.merges.size() * sizeof(int2));
+  std::vector<char> host(bytes, 0);
+  std::copy_n((const char*)v.items.data(), v.items.size() * sizeof(dc::AttnItem), host.data() + at_items);
+  std::copy_n((const char*)v.first.data(), v.first.size() * sizeof(int), host.data() + at_first);
+  std::copy_n((const char*)v.merges.data(), v.merges.size() * sizeof(int2), host.data() + at_merges);
+  auto p = std::make_unique<dc_prompt_plan>();
+  char* block = nullptr;
+  e = cudaMalloc(&block, bytes);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return prompt_cuda(e, "plan allocation");
   }
-  dc_prompt_plan* p = new dc_prompt_plan();
+  e = cudaMemcpy(block, host.data(), bytes, cudaMemcpyHostToDevice);
+  if (e != cudaSuccess) {
+    cudaFree(block);
+    return prompt_cuda(e, "plan upload");
+  }
   p->device = dev;
+  p->num_sms = sms;
   p->q_heads = q_heads;
   p->kv_heads = kv_heads;
   p->head_dim = head_dim;
   p->q_tokens = qt;
   p->k_tokens = kt;
-  p->n_items = (int)items.size();
-  p->items = d;
-  *out = p;
+  p->n_items = (int)v.items.size();
+  p->n_merges = (int)v.merges.size();
+  p->n_slots = v.slots;
+  p->prows = v.prows;
+  p->grid = (int)v.first.size() - 1;
+  p->status = (unsigned*)block;
+  p->items = (dc::AttnItem*)(block + at_items);
+  p->first = (int*)(block + at_first);
+  p->merges = (int2*)(block + at_merges);
+  *out = p.release();
   return DC_OK;
 } catch (const std::bad_alloc&) {
   return prompt_fail(DC_ERR_OOM, "host allocation failed");
@@ -151,7 +250,7 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
 dc_status dc_prompt_plan_destroy(dc_prompt_plan* p) {
   if (!p) return DC_OK;
   if (p->magic != dc::kPlanMagic) return DC_ERR_INVALID_ARG;
-  cudaFree(p->items);
+  cudaFree(p->status);
   p->magic = 0;
   delete p;
   return DC_OK;
@@ -167,8 +266,12 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   if (!x.q || !x.out || (p->k_tokens && (!x.k || !x.v))) return prompt_fail(DC_ERR_INVALID_ARG, "NULL pointer");
   const uintptr_t at = (uintptr_t)x.q | (uintptr_t)x.out | (p->k_tokens ? (uintptr_t)x.k | (uintptr_t)x.v : 0);
   const long long strides[] = {x.q_token_stride, x.q_head_stride, x.k_token_stride, x.k_head_stride, x.v_token_stride, x.v_head_stride};
-  for (long long st : strides)
-    if (st < 0 || st % 8 || st >= (1ll << 38)) return prompt_fail(DC_ERR_INVALID_ARG, "strides must be multiples of 8 in [0, 2^38)");
+  const long long counts[] = {p->q_tokens, p->q_heads, p->k_tokens, p->kv_heads, p->k_tokens, p->kv_heads};
+  for (int i = 0; i < 6; ++i)  // (the stride of a dimension of one says nothing)
+    if (counts[i] > 1 && (strides[i] < 8 || strides[i] % 8 || strides[i] >= (1ll << 38)))
+      return prompt_fail(DC_ERR_INVALID_ARG, "strides must be multiples of 8 in [8, 2^38)");
+  if (x.workspace_bytes < p->workspace() || (p->workspace() && (!x.workspace || (uintptr_t)x.workspace & 15)))
+    return prompt_fail(DC_ERR_INVALID_ARG, "the workspace must hold dc_prompt_workspace bytes, 16-byte aligned");
   if (at & 15) return prompt_fail(DC_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
   int dev = -1;
   cudaError_t e = cudaGetDevice(&dev);
@@ -193,18 +296,55 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   a.scale = x.scale;
   a.c = (float)(1.4426950408889634 * x.scale);
   a.items = p->items;
+  a.first = p->first;
+  a.merges = p->merges;
   a.n_items = p->n_items;
+  a.n_merges = p->n_merges;
+  a.prows = p->prows;
+  a.part = (float*)x.workspace;
+  a.part_ml = (float2*)((float*)x.workspace + (size_t)p->n_slots * p->prows * p->head_dim);
+  a.status = p->status;
+  a.dbg = p->status + 8;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool bf = x.dtype == DC_BF16;
-  if (p->head_dim == 128) {
-    if (bf) dc::prompt_rows_kernel<dc::TypeBf16, 128><<<p->n_items, 256, 0, s>>>(a);
-    else dc::prompt_rows_kernel<dc::TypeHalf, 128><<<p->n_items, 256, 0, s>>>(a);
-  } else {
-    if (bf) dc::prompt_rows_kernel<dc::TypeBf16, 64><<<p->n_items, 256, 0, s>>>(a);
-    else dc::prompt_rows_kernel<dc::TypeHalf, 64><<<p->n_items, 256, 0, s>>>(a);
-  }
-  e = cudaGetLastError();
+  const int D = p->head_dim;
+  dc::AttMaps m;
+  // (no keys at all: every row's result is 0, and the maps of keys are not used)
+  const bool none = p->k_tokens == 0;
+  if (!dc::att_map_q(&m.q, bf, a, D, p->q_tokens, 1) ||
+      !dc::att_map_kv(&m.k, bf, none ? x.q : x.k, D, p->kv_heads, none ? D : a.k_y, none ? 1 : p->k_tokens, none ? D : a.k_t) ||
+      !dc::att_map_kv(&m.v, bf, none ? x.q : x.v, D, p->kv_heads, none ? D : a.v_y, none ? 1 : p->k_tokens, none ? D : a.v_t))
+    return prompt_fail(DC_ERR_INVALID_ARG, "cuTensorMapEncodeTiled rejected the layout of q, k or v");
+  m.kd = m.k;
+  m.vd = m.v;
+  if (D == 128)
+    e = bf ? dc::launch_attend<dc::TypeBf16, 128, false>(m, a, p->grid, p->num_sms, s)
+           : dc::launch_attend<dc::TypeHalf, 128, false>(m, a, p->grid, p->num_sms, s);
+  else
+    e = bf ? dc::launch_attend<dc::TypeBf16, 64, false>(m, a, p->grid, p->num_sms, s)
+           : dc::launch_attend<dc::TypeHalf, 64, false>(m, a, p->grid, p->num_sms, s);
   if (e != cudaSuccess) return prompt_cuda(e, "launch");
+  return DC_OK;
+}
+
+dc_status dc_prompt_workspace(const dc_prompt_plan* p, size_t* bytes) {
+  if (!p || p->magic != dc::kPlanMagic || !bytes) return prompt_fail(DC_ERR_INVALID_ARG, "not a plan");
+  *bytes = p->workspace();
+  return DC_OK;
+}
+
+dc_status dc_prompt_check(const dc_prompt_plan* p, void* stream) {
+  if (!p || p->magic != dc::kPlanMagic) return prompt_fail(DC_ERR_INVALID_ARG, "not a plan");
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+  unsigned st[16] = {};
+  if (e == cudaSuccess) e = cudaMemcpy(st, p->status, sizeof st, cudaMemcpyDeviceToHost);
+  if (e != cudaSuccess) return prompt_cuda(e, "check");
+  if (st[0]) {
+    char buf[160];
+    std::snprintf(buf, sizeof buf, "kernel status word 0x%x (first wait timeout: site %u block %u parity %u info 0x%x)", st[0],
+                  st[9], st[10], st[11], st[12]);
+    return prompt_fail(DC_ERR_DEVICE, buf);
+  }
   return DC_OK;
 }
 

@@ -1,35 +1,47 @@
 // dc_tree.cu -- attention of drafted trees over the rows of a cache (dc_tree_attend).
+#include <algorithm>
+
+#include "dc_attend_kernel.cuh"
 #include "dc_prompt.h"
 
 namespace dc {
-namespace {
 
-// A warp per query row.
-template <int D>
-__global__ void __launch_bounds__(256) tree_rows_kernel(AttnArgs a) {
-  const int lane = threadIdx.x & 31, per = a.nodes * a.G;
-  for (long long u = (long long)blockIdx.x * 8 + threadIdx.x / 32; u < (long long)a.rows * per; u += (long long)gridDim.x * 8) {
-    const int y = (int)(u / per), i = (int)(u % per) / a.G, g = (int)(u % a.G);
-    const int lb = y / a.kvh, head = (y % a.kvh) * a.G + g;
-    uint32_t w[4];
-    const bool used = tree_mask(a.parents + (long long)(lb % a.batch) * a.nodes, i, w);
-    float m, l = 1.f, o[D / 32] = {};
-    if (used)
-      attend_row<TypeBf16, D>(a, a.q + lb * a.q_lb + i * a.q_t + head * a.q_h, a.k + y * a.k_y, a.v + y * a.v_y,
-                              a.kd + (long long)y * a.nodes * D, a.vd + (long long)y * a.nodes * D, 0,
-                              a.rowlen ? a.rowlen[y] : a.n, w, m, l, o);
-    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + lb * a.o_lb + i * a.o_t + head * a.o_h) + lane * (D / 64);
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) to[e] = TypeBf16::pack(o[2 * e] / l, o[2 * e + 1] / l);
+long long tree_plan(AttnArgs* a, int D, int num_sms) {
+  const int tpt = kAttRows / a->G;
+  a->pairs = (a->nodes + 2 * tpt - 1) / (2 * tpt);
+  a->prows = a->nodes <= tpt ? a->nodes * a->G : 256;
+  const long long items = (long long)a->rows * a->pairs;
+  const int tiles = (a->n + kAttTok - 1) / kAttTok + 1;
+  // Parts of a row: as few as fill the SMs evenly. In units of a key tile's two products: a
+  // part costs its tiles (twice with two tiles of queries) and 5 for its start and end, and the
+  // merge of parts 5 more.
+  const double unit = a->nodes <= tpt ? 1.0 : 2.0;
+  double best = 0;
+  a->nsplit = 1;
+  for (int ns = 1; ns <= std::min(tiles, 64); ++ns) {
+    const double rounds = (double)((items * ns + num_sms - 1) / num_sms);
+    const double cost = rounds * ((tiles + ns - 1) / ns * unit + 5.0) + (ns > 1 ? 5.0 : 0.0);
+    if (ns == 1 || cost < best) best = cost, a->nsplit = ns;
   }
+  a->n_items = (int)(items * a->nsplit);
+  a->n_merges = a->nsplit > 1 ? (int)items : 0;
+  return a->nsplit > 1 ? items * a->nsplit : 0;
 }
 
-}  // namespace
-
-cudaError_t launch_tree(const AttnArgs& a, int D, int num_sms, cudaStream_t s) {
-  if (D == 128) tree_rows_kernel<128><<<num_sms * 8, 256, 0, s>>>(a);
-  else tree_rows_kernel<64><<<num_sms * 8, 256, 0, s>>>(a);
-  return cudaGetLastError();
+cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, int num_sms, cudaStream_t s, const char** why) {
+  AttMaps m;
+  const bool ok = att_map_q(&m.q, true, a, D, a.nodes, a.rows / a.kvh) &&
+                  att_map_kv(&m.k, true, a.k, D, a.rows, a.k_y, tokens, a.k_t) &&
+                  att_map_kv(&m.v, true, a.v, D, a.rows, a.v_y, tokens, a.v_t) &&
+                  att_map_kv(&m.kd, true, a.kd, D, a.rows, (long long)a.nodes * D, a.nodes, D) &&
+                  att_map_kv(&m.vd, true, a.vd, D, a.rows, (long long)a.nodes * D, a.nodes, D);
+  if (!ok) {
+    *why = "cuTensorMapEncodeTiled rejected the layout";
+    return cudaErrorInvalidValue;
+  }
+  const int grid = std::min(a.n_items, num_sms);
+  return D == 128 ? launch_attend<TypeBf16, 128, true>(m, a, grid, num_sms, s)
+                  : launch_attend<TypeBf16, 64, true>(m, a, grid, num_sms, s);
 }
 
 }  // namespace dc

@@ -36,7 +36,8 @@ EXPORTS = ["dc_config_default", "dc_cache_create", "dc_cache_destroy", "dc_polic
            "dc_set_row_budgets", "dc_get_row_lengths", "dc_wait_selftest", "dc_selftest_last_error",
            "dc_set_graph_mode", "dc_debug_fail_alloc", "dc_debug_checks", "dc_debug_bounds_selftest",
            "dc_debug_corrupt_guard", "dc_debug_schedule", "dc_tree_attend", "dc_norm_rotate", "dc_rotate_last_error",
-           "dc_prompt_plan_create", "dc_prompt_plan_destroy", "dc_prompt_attend", "dc_prompt_last_error"]
+           "dc_prompt_plan_create", "dc_prompt_plan_destroy", "dc_prompt_attend", "dc_prompt_last_error",
+           "dc_prompt_workspace", "dc_prompt_check"]
 PHASES = ["append", "attend", "stats", "score", "combine", "evict", "full"]
 
 
@@ -64,7 +65,7 @@ class dc_prompt_args(C.Structure):
     _fields_ = [("dtype", C.c_int), ("scale", C.c_float), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("q_token_stride", C.c_longlong), ("q_head_stride", C.c_longlong), ("k_token_stride", C.c_longlong),
                 ("k_head_stride", C.c_longlong), ("v_token_stride", C.c_longlong), ("v_head_stride", C.c_longlong),
-                ("out", C.c_void_p), ("lse", C.c_void_p)]
+                ("out", C.c_void_p), ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 class DCError(RuntimeError):
@@ -121,6 +122,8 @@ def lib():
             L.dc_prompt_plan_create.argtypes = [P, P, I, I, I, I, I, C.POINTER(P)]
             L.dc_prompt_plan_destroy.argtypes = [P]
             L.dc_prompt_attend.argtypes = [P, C.POINTER(dc_prompt_args), P]
+            L.dc_prompt_workspace.argtypes = [P, C.POINTER(S)]
+            L.dc_prompt_check.argtypes = [P, P]
             L.dc_prompt_last_error.argtypes = []
             L.dc_prompt_last_error.restype = C.c_char_p
             L.dc_wait_selftest.argtypes = [C.c_ulonglong, P, P]
@@ -443,12 +446,18 @@ class PromptPlan:
         self.kv_heads, self.head_dim, self.q_heads = kv_heads, head_dim, 4 * kv_heads if q_heads is None else q_heads
         self.q_tokens, self.k_tokens = int(ql.sum(dtype=np.int64)), int(kl.sum(dtype=np.int64))
         p = C.c_void_p()
-        st = lib().dc_prompt_plan_create(ql.ctypes.data_as(C.c_void_p), kl.ctypes.data_as(C.c_void_p), ql.size,
-                                         self.q_heads, kv_heads, head_dim, int(bool(causal)), C.byref(p))
-        if st != DC_OK:
-            raise DCError(st, lib().dc_prompt_last_error().decode())
+        self._ok(lib().dc_prompt_plan_create(ql.ctypes.data_as(C.c_void_p), kl.ctypes.data_as(C.c_void_p), ql.size,
+                                             self.q_heads, kv_heads, head_dim, int(bool(causal)), C.byref(p)))
         self._p = p
         self.device = torch.cuda.current_device()
+        n = C.c_size_t()
+        self._ok(lib().dc_prompt_workspace(p, C.byref(n)))
+        self.workspace_bytes = n.value
+
+    @staticmethod
+    def _ok(st: int) -> None:
+        if st != DC_OK:
+            raise DCError(st, lib().dc_prompt_last_error().decode())
 
     def close(self) -> None:
         if getattr(self, "_p", None):
@@ -484,11 +493,15 @@ class PromptPlan:
         with torch.cuda.device(dev), _on(q.device, stream, q, k, v, out) as s:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
-            a.out, a.lse = _ptr(out), _ptr(lse)
-            st = lib().dc_prompt_attend(self._p, C.byref(a), s)
-        if st != DC_OK:
-            raise DCError(st, lib().dc_prompt_last_error().decode())
+            work = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=q.device) if self.workspace_bytes else None
+            a.out, a.lse, a.workspace, a.workspace_bytes = _ptr(out), _ptr(lse), _ptr(work), self.workspace_bytes
+            self._ok(lib().dc_prompt_attend(self._p, C.byref(a), s))
         return (out, lse) if with_lse else out
+
+    def check(self, stream=None) -> None:
+        """Waits for the stream; raises if a kernel of this plan reported an error."""
+        import torch
+        self._ok(lib().dc_prompt_check(self._p, (stream or torch.cuda.current_stream(self.device)).cuda_stream))
 
 
 class DistillCache:
