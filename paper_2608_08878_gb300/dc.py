@@ -82,6 +82,8 @@ _lock = threading.Lock()
 def lib():
     """Opens libdistillcache.so (raises if it has not been built)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -329,25 +331,27 @@ def _heads(t, name: str, heads: int | None, dim: int | None, dtype, device: int)
     import torch
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise DCError(DC_ERR_INVALID_ARG, f"{name} must be a [tokens][heads][head_dim] tensor")
-    if not t.is_cuda or t.device.index != device:
+    if t.get_device() != device:
         raise DCError(DC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected cuda:{device}")
     if t.dtype != dtype:
         raise DCError(DC_ERR_INVALID_ARG, f"{name} must be {dtype}, got {t.dtype}")
-    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+    T, H, D = t.shape
+    if (heads is not None and H != heads) or (dim is not None and D != dim):
         raise DCError(DC_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}, expected (tokens, {heads}, {dim})")
     st, sh, sd = t.stride()
-    T, H, D = t.shape
     # (the stride of a dimension of one says nothing)
-    st, sh = (st if T > 1 else H * D), (sh if H > 1 else D)
-    if sd != 1 or st % 8 or sh % 8 or st < 0 or sh < 0 or t.data_ptr() % 16:
+    if T <= 1:
+        st = H * D
+    if H <= 1:
+        sh = D
+    p = t.data_ptr()
+    if sd != 1 or st & 7 or sh & 7 or p & 15:
         raise DCError(DC_ERR_INVALID_ARG, f"{name} must start every head on 16 bytes (strides {tuple(t.stride())})")
-    return t.data_ptr(), st, sh
+    return p, st, sh
 
 
-def _fresh(t, name: str, shape):
-    """Checks that the output tensor t, if given, has this shape and no two places for one value."""
-    if t is None:
-        return
+def _fresh(t, name: str, shape) -> None:
+    """Checks that the output tensor t has this shape and no two places for one value."""
     if tuple(t.shape) != tuple(shape):
         raise DCError(DC_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     dims = sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1)
@@ -355,36 +359,35 @@ def _fresh(t, name: str, shape):
         raise DCError(DC_ERR_INVALID_ARG, f"{name}'s elements overlap (strides {tuple(t.stride())})")
 
 
-class _on:
-    """The stream that a handle-free call runs on, made current, so that what the call allocates belongs to it;
-    tensors made on another stream are told that this one uses them."""
-
-    def __init__(self, device, stream, *tensors):
-        import torch
-        if stream is not None and stream.device != device:
-            raise DCError(DC_ERR_INVALID_ARG, f"stream is on {stream.device}, the tensors on {device}")
-        self.stream = stream or torch.cuda.current_stream(device)
-        if stream is not None and stream != torch.cuda.current_stream(device):
+def _run_on(device: int, stream, tensors, call):
+    """call(stream handle) with `device` current, on `stream` or the device's current stream. With a stream given it
+    is made current, so that what the call allocates belongs to it, and tensors made on another are told that
+    this one uses them."""
+    import torch
+    if stream is None:
+        if torch.cuda.current_device() == device:
+            return call(torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(device):
+            return call(torch.cuda.current_stream(device).cuda_stream)
+    if stream.device.index != device:
+        raise DCError(DC_ERR_INVALID_ARG, f"stream is on {stream.device}, the tensors on cuda:{device}")
+    with torch.cuda.device(device):
+        if stream != torch.cuda.current_stream(device):
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
-        self.ctx = torch.cuda.stream(self.stream)
-
-    def __enter__(self):
-        self.ctx.__enter__()
-        return self.stream.cuda_stream
-
-    def __exit__(self, *a):
-        self.ctx.__exit__(*a)
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
 
 
 def _dtype16(t, name: str) -> int:
     import torch
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.bfloat16, torch.float16):
+    dtype = getattr(t, "dtype", None)
+    if dtype != torch.bfloat16 and dtype != torch.float16:
         raise DCError(DC_ERR_INVALID_ARG, f"{name} must be a bfloat16 or float16 tensor")
     if not t.is_cuda:
         raise DCError(DC_ERR_INVALID_ARG, f"{name} must be a CUDA tensor")
-    return 0 if t.dtype == torch.bfloat16 else 1
+    return 0 if dtype == torch.bfloat16 else 1
 
 
 def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps: float = 1e-6, norm: bool = True,
@@ -398,37 +401,41 @@ def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps:
     q_out, k_out: where the results go, of q's and k's shape (views too, so that keys can go straight into
     `append`'s [kv_heads][tokens][d]; q and k themselves: in place). Returns (q_out, k_out)."""
     import torch
-    a = dc_rotate_args()
-    a.dtype = _dtype16(q, "q")
-    dev = q.device.index
-    a.q, a.q_token_stride, a.q_head_stride = _heads(q, "q", None, None, q.dtype, dev)
-    T, a.q_heads, d = q.shape
-    a.k, a.k_token_stride, a.k_head_stride = _heads(k, "k", None, d, q.dtype, dev)
+    kind = _dtype16(q, "q")
+    dtype, dev = q.dtype, q.get_device()
+    at_q = _heads(q, "q", None, None, dtype, dev)
+    T, hq, d = q.shape
+    at_k = _heads(k, "k", None, d, dtype, dev)
+    hk = k.shape[1]
     if k.shape[0] != T:
         raise DCError(DC_ERR_INVALID_ARG, f"q has {T} tokens, k {k.shape[0]}")
-    a.tokens, a.kv_heads, a.head_dim = T, k.shape[1], d
-    a.norm, a.interleaved, a.eps = int(bool(norm)), int(bool(interleaved)), eps
-    a.positions = _arg(positions, "positions", torch.int32, T, device=dev)
+    pos = _arg(positions, "positions", torch.int32, T, device=dev)
     if not isinstance(inv_freq, torch.Tensor):
         raise DCError(DC_ERR_INVALID_ARG, "inv_freq must be a torch tensor")
-    a.rotary_dim = 2 * inv_freq.numel()
-    a.inv_freq = _arg(inv_freq, "inv_freq", torch.float32, inv_freq.numel(), device=dev)
-    a.q_weight = None if q_weight is None else _arg(q_weight, "q_weight", torch.float32, d, device=dev)
-    a.k_weight = None if k_weight is None else _arg(k_weight, "k_weight", torch.float32, d, device=dev)
-    outs = {"q_out": q_out, "k_out": k_out}
-    for name, like in (("q_out", q), ("k_out", k)):
-        if outs[name] is not None:
-            _heads(outs[name], name, like.shape[1], d, q.dtype, dev)
-            _fresh(outs[name], name, like.shape)
-    with torch.cuda.device(dev), _on(q.device, stream, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out) as s:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        a.q_out, a.q_out_token_stride, a.q_out_head_stride = _heads(q_out, "q_out", a.q_heads, d, q.dtype, dev)
-        a.k_out, a.k_out_token_stride, a.k_out_head_stride = _heads(k_out, "k_out", a.kv_heads, d, q.dtype, dev)
-        st = lib().dc_norm_rotate(C.byref(a), s)
-    if st != DC_OK:
-        raise DCError(st, lib().dc_rotate_last_error().decode())
-    return q_out, k_out
+    pairs = inv_freq.numel()
+    freq = _arg(inv_freq, "inv_freq", torch.float32, pairs, device=dev)
+    wq = None if q_weight is None else _arg(q_weight, "q_weight", torch.float32, d, device=dev)
+    wk = None if k_weight is None else _arg(k_weight, "k_weight", torch.float32, d, device=dev)
+    if q_out is not None:
+        to_q = _heads(q_out, "q_out", hq, d, dtype, dev)
+        _fresh(q_out, "q_out", q.shape)
+    if k_out is not None:
+        to_k = _heads(k_out, "k_out", hk, d, dtype, dev)
+        _fresh(k_out, "k_out", k.shape)
+
+    def call(s):
+        qo = torch.empty((T, hq, d), dtype=dtype, device=q.device) if q_out is None else q_out
+        ko = torch.empty((T, hk, d), dtype=dtype, device=q.device) if k_out is None else k_out
+        tq = (qo.data_ptr(), hq * d, d) if q_out is None else to_q
+        tk = (ko.data_ptr(), hk * d, d) if k_out is None else to_k
+        a = dc_rotate_args(T, hq, hk, d, 2 * pairs, kind, 1 if norm else 0, 1 if interleaved else 0, eps, pos, freq, wq, wk,
+                           at_q[0], at_k[0], tq[0], tk[0], at_q[1], at_q[2], at_k[1], at_k[2], tq[1], tq[2], tk[1], tk[2])
+        st = lib().dc_norm_rotate(a, s)
+        if st != DC_OK:
+            raise DCError(st, lib().dc_rotate_last_error().decode())
+        return qo, ko
+
+    return _run_on(dev, stream, (q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out), call)
 
 
 class PromptPlan:
@@ -477,26 +484,29 @@ class PromptPlan:
         import torch
         if not self._p:
             raise DCError(DC_ERR_INVALID_ARG, "the plan is closed")
-        a = dc_prompt_args()
-        a.dtype = _dtype16(q, "q")
-        d, dev = self.head_dim, self.device
-        a.q, a.q_token_stride, a.q_head_stride = _heads(q, "q", self.q_heads, d, q.dtype, dev)
-        a.k, a.k_token_stride, a.k_head_stride = _heads(k, "k", self.kv_heads, d, q.dtype, dev)
-        a.v, a.v_token_stride, a.v_head_stride = _heads(v, "v", self.kv_heads, d, q.dtype, dev)
+        kind = _dtype16(q, "q")
+        dtype, d, dev = q.dtype, self.head_dim, self.device
+        at_q = _heads(q, "q", self.q_heads, d, dtype, dev)
+        at_k = _heads(k, "k", self.kv_heads, d, dtype, dev)
+        at_v = _heads(v, "v", self.kv_heads, d, dtype, dev)
         if q.shape[0] != self.q_tokens or k.shape[0] != self.k_tokens or v.shape[0] != self.k_tokens:
             raise DCError(DC_ERR_INVALID_ARG, f"q, k and v have {q.shape[0]}, {k.shape[0]} and {v.shape[0]} tokens, the plan "
                           f"{self.q_tokens} and {self.k_tokens}")
-        a.scale = 1.0 / d ** 0.5 if scale is None else scale
         if out is not None:
             _fresh(out, "out", q.shape)
-            _arg(out, "out", q.dtype, q.numel(), device=dev)
-        with torch.cuda.device(dev), _on(q.device, stream, q, k, v, out) as s:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+            _arg(out, "out", dtype, q.numel(), device=dev)
+
+        def call(s):
+            o = torch.empty(q.shape, dtype=dtype, device=q.device) if out is None else out
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
-            work = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=q.device) if self.workspace_bytes else None
-            a.out, a.lse, a.workspace, a.workspace_bytes = _ptr(out), _ptr(lse), _ptr(work), self.workspace_bytes
-            self._ok(lib().dc_prompt_attend(self._p, C.byref(a), s))
-        return (out, lse) if with_lse else out
+            need = self.workspace_bytes
+            work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+            a = dc_prompt_args(kind, 1.0 / d ** 0.5 if scale is None else scale, at_q[0], at_k[0], at_v[0], at_q[1], at_q[2],
+                               at_k[1], at_k[2], at_v[1], at_v[2], o.data_ptr(), _ptr(lse), _ptr(work), need)
+            self._ok(lib().dc_prompt_attend(self._p, a, s))
+            return (o, lse) if with_lse else o
+
+        return _run_on(dev, stream, (q, k, v, out), call)
 
     def check(self, stream=None) -> None:
         """Waits for the stream; raises if a kernel of this plan reported an error."""
@@ -666,8 +676,11 @@ class DistillCache:
         pk = _arg(k_draft, "k_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         pv = _arg(v_draft, "v_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         if out is None:
-            with torch.cuda.stream(self.stream):
+            if torch.cuda.current_stream(self.device) == self.stream:
                 out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+            else:  # (what the cache's stream writes belongs to that stream)
+                with torch.cuda.stream(self.stream):
+                    out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
         po = _arg(out, "out", torch.bfloat16, n * self.q_heads, device=self.device)
         self._check(lib().dc_tree_attend(self._h, pq, pk, pv, pp, T, po))
         return out
