@@ -134,6 +134,15 @@ def test_zeros_and_values_that_are_not_finite():
     assert bool(torch.isfinite(qo[1, 0][other]).all()) and bool(torch.isnan(qo[1, 0][~other]).all())
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_dims_past_the_rotated_ones_keep_to_themselves(interleaved):
+    q, k, pos, f, w = inputs(3, 2, 1, 96, 32, BF)
+    q[0, 0, 40], q[1, 1, 95], q[2, 0, 33] = math.nan, math.inf, -math.inf
+    qo, _ = dc.norm_rotate(q, k, pos, f, norm=False, interleaved=interleaved)
+    assert torch.allclose(qo[..., 32:], q[..., 32:], rtol=0, atol=0, equal_nan=True)
+    assert bool(torch.isfinite(qo[..., :32]).all())
+
+
 def test_tiny_and_huge_heads_keep_their_norm():
     """Squares below the normal range and above 2^127 of the type's own range: bf16 heads of 1e-18 and 1e17."""
     q, k, pos, f, w = inputs(8, 2, 1, 128, 128, BF)
