@@ -41,7 +41,7 @@ struct AttnArgs {
   float2* part_ml;
   int prows;
   // trees
-  int n, nodes, batch, rows, pairs, nsplit;
+  int n, nodes, batch, rows, pairs, tiles, grid;
   const int* rowlen;         // each row's length, or null (n)
   const int* parents;        // [batch][nodes]
   unsigned* status;
@@ -57,6 +57,8 @@ struct AttnItem {
   int j0, j1;     // key tiles
   int slot;       // where a part of the keys leaves its partial result; -1: all keys
   int alt;        // one tile of query rows only
+  int eA, eB;     // key tiles that A's and B's rows see: below these
+  int lowA, lowB; // what A's and B's first row sees, the least of their rows
 };
 constexpr int kSeesAll = 1 << 30;
 

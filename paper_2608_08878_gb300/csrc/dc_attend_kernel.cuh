@@ -4,17 +4,19 @@
 // One persistent CTA per SM takes work items in turn: two tiles of 128 query rows (A and
 // B) of one KV head over a run of key tiles of 128 tokens. Warp roles (384 threads):
 //   warps 0-3, 4-7  softmax warpgroups of tiles A and B, one query row (TMEM lane) a thread;
-//   warp 8          producer: query tiles, then K and V tiles in the order in which the
-//                   products take them, by TMA through one ring of stages;
+//   warp 8          producer: publishes the items to the other warps, loads the query tiles,
+//                   then K and V tiles in the order in which the products take them, by TMA
+//                   through one ring of stages;
 //   warp 9          MMA issuer (one lane):
 //                     S_X  = Q_X K^T     [128 rows x 128 keys]   from shared memory
 //                     O_X += P_X V       [128 rows x D]          P_X from TMEM
-//   warps 10, 11    idle (the third warpgroup gives up registers as a whole)
+//   warps 10, 11    look over the values of key tiles that are masked in part.
 // TMEM columns: S_A [0, 128), S_B [128, 256), O_A [256, 256 + D), O_B [384, 384 + D). A
 // warpgroup reads its S (the whole row in registers), writes the weights P over its
 // first 64 columns in the inputs' type, and the second product reads them there. The
 // issuer sends S_X of the next key tile right behind O_X of this one, so that one
-// warpgroup's softmax runs under the other's products.
+// warpgroup's softmax runs under the other's products. P goes in two halves, each with its
+// own barrier: the product with the first half's values starts while the second is computed.
 //
 // Running softmax: m is a row's reference, not always its maximum: it follows the maximum
 // only where that is more than 2^8 above it in weights, so that O is seldom rescaled (P
@@ -26,14 +28,17 @@
 // tiles to A and B in turn, both on the same queries, and join the two results at the end:
 // the pipeline is the same.
 //
-// A masked key has weight 0, but 0 times a value that is not finite is NaN: the values of key
-// tiles that are masked in part are looked over in shared memory, and a tile of rows that
-// meets such a value is recomputed by attend_row, which reads only what a row sees.
+// A masked key has weight 0, but 0 times a value that is not finite is NaN: warps 10 and 11 look
+// over the values that some row of the tile must not see, in shared memory, before their stage
+// is released, and a tile of rows that meets such a value is recomputed by attend_row, which
+// reads only what a row sees.
 //
-// Barriers: every wait is bounded. A wait that gives up sets *abort; the softmax
-// warps then go on without waiting (their loops and named barriers match all the same), the
-// producer and the issuer stop, wait for what they have in flight, and the status word
-// says so.
+// Results go through shared memory, 32 dims of a warp's 32 rows at a time, so that each row's 64
+// bytes leave together (a thread writing its own row cost 5000 to 7000 cycles an item).
+//
+// Barriers: every wait is bounded, and the roles meet at mbarriers only. A wait that gives up
+// sets *abort; every warp then leaves its loop, the producer and the issuer wait for what they
+// have in flight, and the status word says so.
 #pragma once
 
 #include <cuda.h>
@@ -52,63 +57,67 @@ constexpr int kAttThreads = 384;
 // 216 + 72 = 3 x 168). A softmax thread holds its whole row of S.
 constexpr int kAttRegsRow = 216, kAttRegsIssue = 72;
 constexpr int kAttCols = 512;
+constexpr int kItemRing = 4;  // items published ahead
 
 template <int D>
 struct AttSmem {
   static constexpr int TILE = 128 * D * 2;
-  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int STAGES = D == 128 ? 4 : 8;
   static constexpr int Q = 0;  // two query tiles
   static constexpr int RING = 2 * TILE;
-  static constexpr int MISC = RING + STAGES * TILE;
-  static constexpr int XCH = MISC + 512;  // float2 [2][128]: m, l of both tiles
+  static constexpr int OUT = RING + STAGES * TILE;  // 4 KB a softmax warp
+  static constexpr int MISC = OUT + 8 * 4096;       // barriers
+  static constexpr int ITEM = MISC + 512;           // AttnItem [4]
+  static constexpr int FLAG = ITEM + kItemRing * 64;  // int [4][2]: what warps 10 and 11 found
+  static constexpr int XCH = MISC + 1024;           // float2 [2][128]: m, l of both tiles
   static constexpr int BYTES = XCH + 2048;
   static_assert(BYTES <= 232448, "more shared memory than a CTA may have");
 };
 
 __device__ __forceinline__ AttnItem load_item(const AttnArgs& a, int i) {
   const int4* p = reinterpret_cast<const int4*>(a.items + i);
-  const int4 x = __ldg(p), y = __ldg(p + 1), z = __ldg(p + 2);
-  return AttnItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+  const int4 x = __ldg(p), y = __ldg(p + 1), z = __ldg(p + 2), w = __ldg(p + 3);
+  return AttnItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w, w.x, w.y, w.z, w.w};
 }
 
-// Work item i of a tree call: row, pair of query tiles, and share of its key tiles (the
-// cached tokens', then the drafted ones').
-__device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int i) {
-  const int tpt = kAttRows / a.G, sp = i % a.nsplit, rest = i / a.nsplit;
+// Trees: the key tiles of all items (rows' pairs of query tiles, a.tiles key tiles each: the
+// cached tokens', then the drafted ones'; rows may have fewer) in one line, of which CTA b of
+// `grid` takes the b-th equal part.
+__host__ __device__ inline long long tree_from(const AttnArgs& a, int b) {
+  return (long long)a.n_items * a.tiles * b / a.grid;
+}
+
+// The item that starts at place `at` of that line, as far as it goes before `end`.
+__device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int b, long long at, long long end) {
+  const int tpt = kAttRows / a.G, i = (int)(at / a.tiles), j0 = (int)(at - (long long)i * a.tiles);
+  const int j1 = (int)(end - at < a.tiles - j0 ? j0 + (end - at) : a.tiles);
   AttnItem it;
-  it.y = rest / a.pairs;
+  it.y = i / a.pairs;
   it.lb = it.y / a.kvh;
   it.h = it.y % a.kvh;
-  it.t0 = rest % a.pairs * 2 * tpt;
+  it.t0 = i % a.pairs * 2 * tpt;
   it.tend = a.nodes;
   it.k0 = 0;
   it.klen = a.rowlen ? __ldg(a.rowlen + it.y) : a.n;
   it.off = kSeesAll;
-  const int tiles = (it.klen + kAttTok - 1) / kAttTok + 1;
-  it.j0 = (int)((long long)tiles * sp / a.nsplit);
-  it.j1 = (int)((long long)tiles * (sp + 1) / a.nsplit);
-  it.slot = a.nsplit > 1 ? i : -1;
+  const int own = (it.klen + kAttTok - 1) / kAttTok + 1;
+  it.j0 = min(j0, own);
+  it.j1 = min(j1, own);
+  // a CTA has at most two parts of items: the end of one, then the start of another
+  it.slot = j0 == 0 && j1 == a.tiles ? -1 : 2 * b + (j0 == 0 ? 1 : 0);
   it.alt = it.tend - it.t0 <= tpt;
+  it.eA = it.eB = it.j1;
+  it.lowA = it.lowB = it.klen;
   return it;
 }
 
 // An item's steps: key tile of step i, and which of A (1) and B (2) take it.
 template <bool TREE>
 struct Steps {
-  int n, j0, j1, eA, eB, alt, look;
-  __device__ __forceinline__ Steps(const AttnArgs& a, const AttnItem& it) {
-    j0 = it.j0;
-    j1 = it.j1;
-    n = j1 - j0;
-    alt = it.alt;
-    look = alt ? 2 : 1;
-    eA = eB = j1;
-    if (!TREE && !alt) {
-      const int tpt = kAttRows / a.G;
-      eA = (att_limit(it, it.t0 + tpt - 1) + kAttTok - 1) / kAttTok;
-      eB = (att_limit(it, min(it.tend, it.t0 + 2 * tpt) - 1) + kAttTok - 1) / kAttTok;
-    }
-  }
+  int n, j0, j1, eA, eB, lowA, lowB, alt, look, draft;
+  __device__ __forceinline__ Steps(const AttnItem& it)
+      : n(it.j1 - it.j0), j0(it.j0), j1(it.j1), eA(it.eA), eB(it.eB), lowA(it.lowA), lowB(it.lowB), alt(it.alt),
+        look(it.alt ? 2 : 1), draft(TREE ? (it.klen + kAttTok - 1) / kAttTok : -1) {}
   // the tiles that may be masked come first in prompts, last in trees
   __device__ __forceinline__ int tile(int i) const { return TREE ? j0 + i : j1 - 1 - i; }
   __device__ __forceinline__ int who(int i) const {
@@ -118,13 +127,20 @@ struct Steps {
     const int j = tile(i);
     return (j < eA ? 1 : 0) | (j < eB ? 2 : 0);
   }
+  // whether some row of tile A (x = 0) or B must not see some key of step i's tile
+  __device__ __forceinline__ bool masked(int i, int x) const {
+    const int j = tile(i);
+    return (TREE && j == draft) || (j + 1) * kAttTok > (x ? lowB : lowA);
+  }
+  // of those that take the step
+  __device__ __forceinline__ int masked(int i) const {
+    const int w = who(i);
+    return (w & 1 && masked(i, 0) ? 1 : 0) | (w & 2 && masked(i, 1) ? 2 : 0);
+  }
   // steps of A (x = 0) or B
   __device__ __forceinline__ int count(int x) const {
     return alt ? (n + 1 - x) / 2 : max(0, min(x ? eB : eA, j1) - j0);
   }
-  // where V of step i comes in the item's loads: K of the first `look` steps, then V of
-  // each step and K of the step `look` later
-  __device__ __forceinline__ int v_at(int i) const { return i + min(n, look + i); }
 };
 
 __device__ __forceinline__ uint32_t below(int count, int word) {
@@ -153,19 +169,60 @@ struct Mma<TypeHalf> {
   }
 };
 
-// One row's result: o / l and lse, or, of a part of the keys, o, m and l.
-template <class T, int D>
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Pairs of 32-bit values.
+__device__ __forceinline__ uint64_t pair2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair2(uint64_t x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Where one row's result goes: o / l and lse, or, of a part of the keys, o, m and l.
 struct RowOut {
-  uint32_t* out;   // the row's output, as 32-bit words
+  uint8_t* out;    // the row's output, or its place in the partial results
   float* lse;      // or null
-  float* part;     // the row's place in the partial results, or null
-  float2* part_ml;
+  float2* part_ml; // or null: all keys
   bool sees;       // false: o = 0, lse = -infinity
   __device__ __forceinline__ void stats(const AttnArgs& a, float m, float l) const {
-    if (part) *part_ml = sees ? make_float2(m, l) : make_float2(-INFINITY, -1.f);
+    if (part_ml) *part_ml = sees ? make_float2(m, l) : make_float2(-INFINITY, -1.f);
     else if (lse) *lse = sees ? fmaf(m, a.scale, logf(l)) : -INFINITY;
   }
 };
+
+// A warp's 32 rows of C 16-byte chunks from its buffer (row r's chunk e at r * C + (e ^ (r % C)))
+// to `to` of each row, where `on`.
+template <int C>
+__device__ __forceinline__ void flush_rows(const uint4* buf, uint8_t* to, bool on) {
+  const int lane = threadIdx.x & 31, e = lane % C;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int r = i * (32 / C) + lane / C;
+    const uint4 v = buf[r * C + (e ^ (r % C))];
+    uint8_t* p = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), r));
+    if (__shfl_sync(0xffffffffu, (int)on, r)) *reinterpret_cast<uint4*>(p + e * 16) = v;
+  }
+  __syncwarp();
+}
 
 template <class T, int D, bool TREE>
 __global__ void __launch_bounds__(kAttThreads, 1)
@@ -182,24 +239,34 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     return;
   }
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + L::MISC);
-  uint64_t *b_full = bar, *b_empty = bar + ST, *b_qfull = bar + 2 * ST, *b_qempty = b_qfull + 1, *b_s = b_qfull + 2,
-           *b_p = b_qfull + 4, *b_o = b_qfull + 6, *b_drain = b_qfull + 8;
+  uint64_t *b_full = bar, *b_empty = bar + 8, *b_qfull = bar + 16, *b_qempty = bar + 17, *b_s = bar + 18,
+           *b_p = bar + 20 /* [X][half] */, *b_o = bar + 24, *b_drain = bar + 26, *b_item = bar + 27, *b_free = bar + 31,
+           *b_look = bar + 35, *b_x = bar + 39;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::MISC + 400);
   volatile int* abort = reinterpret_cast<int*>(smem + L::MISC + 404);
+  AttnItem* ring = reinterpret_cast<AttnItem*>(smem + L::ITEM);
+  volatile int* flags = reinterpret_cast<int*>(smem + L::FLAG);
   float2* xch = reinterpret_cast<float2*>(smem + L::XCH);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < ST; ++s) {
       mbar_init(&b_full[s], 1);
-      mbar_init(&b_empty[s], 1);
+      mbar_init(&b_empty[s], 3);  // the issuer's commit, warps 10 and 11
     }
     mbar_init(b_qfull, 1);
     mbar_init(b_qempty, 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(&b_s[x], 1);
-      mbar_init(&b_p[x], 4);
+      mbar_init(&b_p[2 * x], 4);
+      mbar_init(&b_p[2 * x + 1], 4);
       mbar_init(&b_o[x], 1);
+      mbar_init(&b_x[x], 8);
+    }
+    for (int e = 0; e < kItemRing; ++e) {
+      mbar_init(&b_item[e], 1);
+      mbar_init(&b_free[e], 11);  // softmax warps, issuer, warps 10 and 11
+      mbar_init(&b_look[e], 2);
     }
     mbar_init(b_drain, 1);
     *abort = 0;
@@ -213,152 +280,238 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-
-  int i0, i1, istep;
-  if (TREE) {
-    i0 = blockIdx.x;
-    i1 = a.n_items;
-    istep = gridDim.x;
-  } else {
-    i0 = __ldg(a.first + blockIdx.x);
-    i1 = __ldg(a.first + blockIdx.x + 1);
-    istep = 1;
-  }
   grid_dep_launch();  // the partial results' merge, if any, may get ready
-  auto item = [&](int i) { return TREE ? tree_item(a, i) : load_item(a, i); };
   const int tpt = kAttRows / a.G;
+
+  // The published item number k, or false: no more, or a wait gave up.
+  auto take = [&](int k, AttnItem& it, unsigned site) {
+    const int e = k % kItemRing;
+    if (!mbar_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k)) return false;
+    const int4* p = reinterpret_cast<const int4*>(ring + e);
+    const int4 x = p[0], y = p[1], z = p[2], w = p[3];
+    it = AttnItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w, w.x, w.y, w.z, w.w};
+    return it.y >= 0;
+  };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kAttRegsIssue));
     if (warp == 8) {
-    // ------------------------------------------------------------ producer
-    if (elect_one()) {
-      const uint64_t pol = TREE ? l2_evict_first_policy() : l2_evict_normal_policy();
-      const uint32_t qbytes = (uint32_t)(tpt * a.G) * (uint32_t)D * 2u;
-      int g = 0, items = 0, q_sent = 0;
-      for (int ii = i0; ii < i1 && !*abort; ii += istep) {
-        const AttnItem it = item(ii);
-        const Steps<TREE> st(a, it);
-        if (st.n == 0) continue;
-        if (!mbar_wait(b_qempty, (items & 1) ^ 1, abort, a.dbg, 201u, (unsigned)ii)) break;
-        mbar_expect_tx(b_qfull, st.alt ? qbytes : 2 * qbytes);
-        for (int x = 0; x < (st.alt ? 1 : 2); ++x)
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_5d(smem + L::Q + x * L::TILE + c * 16384, &tmQ, c * 64, 0, it.h, it.t0 + x * tpt, it.lb, b_qfull);
-        q_sent = ++items;
-        const int draft = TREE ? (it.klen + kAttTok - 1) / kAttTok : -1;
-        auto load = [&](int j, bool v) {
-          const int s = g % ST;
-          if (!mbar_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, a.dbg, 202u, (unsigned)g)) return;
-          mbar_expect_tx(&b_full[s], L::TILE);
-          const bool d = TREE && j == draft;
-          const CUtensorMap* tm = d ? (v ? &tmVD : &tmKD) : v ? &tmV : &tmK;
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(smem + L::RING + s * L::TILE + c * 16384, tm, c * 64, it.y, d ? 0 : it.k0 + j * kAttTok,
-                        &b_full[s], pol);
+      // ---------------------------------------------------------- producer
+      if (elect_one()) {
+        const uint64_t pol = TREE ? l2_evict_first_policy() : l2_evict_normal_policy();
+        const uint32_t qbytes = (uint32_t)(tpt * a.G) * (uint32_t)D * 2u;
+        int g = 0, sent = 0;
+        long long at = 0, end = 0;
+        if (TREE) {
+          at = tree_from(a, blockIdx.x);
+          end = tree_from(a, blockIdx.x + 1);
+        } else {
+          at = __ldg(a.first + blockIdx.x);
+          end = __ldg(a.first + blockIdx.x + 1);
+        }
+        AttnItem next{};
+        auto fetch = [&] {
+          if (at >= end) {
+            next.y = -1;
+          } else if (TREE) {
+            next = tree_item(a, blockIdx.x, at, end);
+            at = (at / a.tiles + 1) * a.tiles;
+          } else {
+            next = load_item(a, (int)at);
+            ++at;
+          }
+        };
+        fetch();
+        for (int k = 0; !*abort; ++k) {
+          const AttnItem it = next;
+          const int e = k % kItemRing;
+          if (!mbar_wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, abort, a.dbg, 200u, (unsigned)k)) break;
+          int4* p = reinterpret_cast<int4*>(ring + e);
+          p[0] = make_int4(it.y, it.h, it.lb, it.t0);
+          p[1] = make_int4(it.tend, it.k0, it.klen, it.off);
+          p[2] = make_int4(it.j0, it.j1, it.slot, it.alt);
+          p[3] = make_int4(it.eA, it.eB, it.lowA, it.lowB);
+          mbar_arrive(&b_item[e]);
+          if (it.y < 0) break;
+          const Steps<TREE> st(it);
+          fetch();
+          if (st.n == 0) continue;
+          if (!mbar_wait(b_qempty, (sent & 1) ^ 1, abort, a.dbg, 201u, (unsigned)k)) break;
+          mbar_expect_tx(b_qfull, st.alt ? qbytes : 2 * qbytes);
+          for (int x = 0; x < (st.alt ? 1 : 2); ++x)
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_5d(smem + L::Q + x * L::TILE + c * 16384, &tmQ, c * 64, 0, it.h, it.t0 + x * tpt, it.lb, b_qfull);
+          ++sent;
+          auto load = [&](int j, bool v) {
+            const int s = g % ST;
+            if (!mbar_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, a.dbg, 202u, (unsigned)g)) return;
+            mbar_expect_tx(&b_full[s], L::TILE);
+            const bool d = TREE && j == st.draft;
+            const CUtensorMap* tm = d ? (v ? &tmVD : &tmKD) : v ? &tmV : &tmK;
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_3d(smem + L::RING + s * L::TILE + c * 16384, tm, c * 64, it.y, d ? 0 : it.k0 + j * kAttTok,
+                          &b_full[s], pol);
+            ++g;
+          };
+          for (int i = 0; i < st.look && i < st.n; ++i) load(st.tile(i), false);
+          for (int i = 0; i < st.n && !*abort; ++i) {
+            load(st.tile(i), true);
+            if (i + st.look < st.n) load(st.tile(i + st.look), false);
+          }
+        }
+        // every issued load must land before the CTA may exit
+        for (int t = g - ST < 0 ? 0 : g - ST; t < g; ++t) mbar_wait_drain(&b_full[t % ST], (t / ST) & 1);
+        if (sent) mbar_wait_drain(b_qfull, (sent - 1) & 1);
+      }
+      __syncwarp();
+    } else if (warp == 9) {
+      // ---------------------------------------------------------- MMA issuer
+      if (elect_one()) {
+        const uint32_t q_lo = sdesc_lo(smem_u32(smem + L::Q), 16), k_lo = sdesc_lo(smem_u32(smem + L::RING), 16),
+                       v_lo = sdesc_lo(smem_u32(smem + L::RING), 16384);
+        constexpr uint32_t hi = sdesc_hi(1024, 2);
+        constexpr uint32_t id_s = Mma<T>::id(128, 0), id_o = Mma<T>::id(D, 1);
+        int g = 0, items = 0;
+        unsigned np0 = 0, np1 = 0;  // P tiles taken of A and B
+        bool ok = true;
+        AttnItem it;
+        for (int k = 0; ok && take(k, it, 203u); ++k) {
+          const Steps<TREE> st(it);
+          if (st.n == 0) {
+            mbar_arrive(&b_free[k % kItemRing]);
+            continue;
+          }
+          ok = mbar_wait(b_qfull, items & 1, abort, a.dbg, 204u, (unsigned)k);
+          if (!ok) break;
+          ++items;
+          auto full = [&](int at) { return mbar_wait(&b_full[at % ST], (at / ST) & 1, abort, a.dbg, 205u, (unsigned)at); };
+          auto s_mma = [&](int x, int at) {
+            const uint32_t klo = k_lo + (uint32_t)(at % ST) * (L::TILE >> 4);
+            const uint32_t qlo = q_lo + (st.alt ? 0u : (uint32_t)x * (L::TILE >> 4));
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t off = ((uint32_t)(ks >> 2) * 16384u + (uint32_t)(ks & 3) * 32u) >> 4;
+              mma_bf16_lo(tmem + x * 128, qlo + off, hi, klo + off, hi, id_s, ks > 0);
+            }
+            mma_commit(&b_s[x]);
+          };
+          auto release = [&](int at) { mma_commit(&b_empty[at % ST]); };
+          for (int i = 0; i < st.look && i < st.n; ++i) {
+            ok = full(g);
+            if (!ok) break;
+            tc_fence_after();
+            const int w = st.who(i);
+            if (w & 1) s_mma(0, g);
+            if (w & 2) s_mma(1, g);
+            release(g);
+            ++g;
+          }
+          if (!ok) break;
+          if (st.look >= st.n) mma_commit(b_qempty);
+          int left0 = st.count(0), left1 = st.count(1);  // steps to come
+          bool fresh0 = true, fresh1 = true;
+          for (int i = 0; i < st.n; ++i) {
+            const int w = st.who(i), w2 = st.who(i + st.look), vat = g, kat = g + 1;
+            ok = full(vat);
+            if (!ok) break;
+            bool have_k = false;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              if (w >> x & 1) {
+                unsigned& np = x ? np1 : np0;
+                bool& fresh = x ? fresh1 : fresh0;
+                const uint32_t vlo = v_lo + (uint32_t)(vat % ST) * (L::TILE >> 4);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  ok = ok && mbar_wait(&b_p[2 * x + h], np & 1, abort, a.dbg, 206u, (unsigned)k);
+                  if (!ok) break;
+                  tc_fence_after();
+#pragma unroll
+                  for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
+                    mma_f16_ts_lo(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, vlo + ks * (2048u >> 4), hi, id_o,
+                                  (!fresh || ks > 0) ? 1u : 0u);
+                }
+                if (!ok) break;
+                ++np;
+                fresh = false;
+                if (--(x ? left1 : left0) == 0) mma_commit(&b_o[x]);
+              }
+              if (w2 >> x & 1) {
+                if (!have_k) {
+                  ok = full(kat);
+                  if (!ok) break;
+                  have_k = true;
+                }
+                tc_fence_after();
+                s_mma(x, kat);
+              }
+            }
+            if (!ok) break;
+            release(vat);
+            ++g;
+            if (i + st.look < st.n) {
+              release(kat);
+              ++g;
+              if (i + st.look == st.n - 1) mma_commit(b_qempty);
+            }
+          }
+          if (ok) mbar_arrive(&b_free[k % kItemRing]);
+        }
+        // all issued MMAs complete before TMEM is released
+        mma_commit(b_drain);
+        mbar_wait_drain(b_drain, 0);
+      }
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------- values of partly masked tiles
+      // (These warps wait for and release every load, so that a stage's phase cannot pass them by,
+      // nor they it: a wait for a parity is sound only one phase away.)
+      int g = 0;
+      AttnItem it;
+      for (int k = 0; __all_sync(0xffffffffu, take(k, it, 207u)); ++k) {
+        const Steps<TREE> st(it);
+        int found = 0;
+        bool ok = true;
+        auto pass = [&](int i) {  // i >= 0: V of step i, else some K
+          ok = __all_sync(0xffffffffu, ok && mbar_wait(&b_full[g % ST], (g / ST) & 1, abort, a.dbg, 208u, (unsigned)g));
+          const int mk = ok && i >= 0 ? st.masked(i) : 0;
+          if (mk) {
+            // the keys that some row must not see
+            const int j = st.tile(i);
+            int lo = max(0, min(mk & 1 ? st.lowA : kSeesAll, mk & 2 ? st.lowB : kSeesAll) - j * kAttTok), hi = kAttTok;
+            if (TREE && j == st.draft) lo = 0, hi = a.nodes;
+            uint32_t acc[4] = {};
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+              const uint4* vt = reinterpret_cast<const uint4*>(smem + L::RING + (g % ST) * L::TILE + c * 16384);
+#pragma unroll 4
+              for (int e = lo * 8 + (warp - 10) * 32 + lane; e < hi * 8; e += 64) {
+                const uint4 w = vt[e];
+                acc[0] = Mma<T>::look(w.x, acc[0]);
+                acc[1] = Mma<T>::look(w.y, acc[1]);
+                acc[2] = Mma<T>::look(w.z, acc[2]);
+                acc[3] = Mma<T>::look(w.w, acc[3]);
+              }
+            }
+            if (__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7fff7fffu) != 0u)) found |= mk;
+          }
+          __syncwarp();
+          if (ok && lane == 0) mbar_arrive(&b_empty[g % ST]);
           ++g;
         };
-        for (int i = 0; i < st.look && i < st.n; ++i) load(st.tile(i), false);
-        for (int i = 0; i < st.n && !*abort; ++i) {
-          load(st.tile(i), true);
-          if (i + st.look < st.n) load(st.tile(i + st.look), false);
-        }
-      }
-      // every issued load must land before the CTA may exit
-      for (int t = g - ST < 0 ? 0 : g - ST; t < g; ++t) mbar_wait_drain(&b_full[t % ST], (t / ST) & 1);
-      if (q_sent) mbar_wait_drain(b_qfull, (q_sent - 1) & 1);
-    }
-    __syncwarp();
-  } else if (warp == 9) {
-    // ------------------------------------------------------------ MMA issuer
-    if (elect_one()) {
-      const uint32_t q_lo = sdesc_lo(smem_u32(smem + L::Q), 16), k_lo = sdesc_lo(smem_u32(smem + L::RING), 16),
-                     v_lo = sdesc_lo(smem_u32(smem + L::RING), 16384);
-      constexpr uint32_t hi = sdesc_hi(1024, 2);
-      constexpr uint32_t id_s = Mma<T>::id(128, 0), id_o = Mma<T>::id(D, 1);
-      int g = 0, items = 0;
-      unsigned np0 = 0, np1 = 0;  // P tiles taken of A and B
-      for (int ii = i0; ii < i1 && !*abort; ii += istep) {
-        const AttnItem it = item(ii);
-        const Steps<TREE> st(a, it);
-        if (st.n == 0) continue;
-        if (!mbar_wait(b_qfull, items & 1, abort, a.dbg, 203u, (unsigned)ii)) break;
-        ++items;
-        int gk = g;  // this item's next load among all loads
-        auto full = [&](int at) { return mbar_wait(&b_full[at % ST], (at / ST) & 1, abort, a.dbg, 204u, (unsigned)at); };
-        auto s_mma = [&](int x, int at) {
-          const uint32_t klo = k_lo + (uint32_t)(at % ST) * (L::TILE >> 4);
-          const uint32_t qlo = q_lo + (st.alt ? 0u : (uint32_t)x * (L::TILE >> 4));
-#pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t off = ((uint32_t)(ks >> 2) * 16384u + (uint32_t)(ks & 3) * 32u) >> 4;
-            mma_bf16_lo(tmem + x * 128, qlo + off, hi, klo + off, hi, id_s, ks > 0);
-          }
-          mma_commit(&b_s[x]);
-        };
-        bool ok = true;
-        for (int i = 0; i < st.look && i < st.n && ok; ++i) {
-          ok = full(gk);
-          if (!ok) break;
-          tc_fence_after();
-          const int w = st.who(i);
-          if (w & 1) s_mma(0, gk);
-          if (w & 2) s_mma(1, gk);
-          mma_commit(&b_empty[gk % ST]);
-          ++gk;
-        }
-        if (st.look >= st.n) mma_commit(b_qempty);
-        int left0 = st.count(0), left1 = st.count(1);  // steps to come
-        bool fresh0 = true, fresh1 = true;
+        for (int i = 0; i < st.look && i < st.n; ++i) pass(-1);
         for (int i = 0; i < st.n && ok; ++i) {
-          const int w = st.who(i), w2 = st.who(i + st.look), vat = gk, kat = gk + 1;
-          ok = full(vat);
-          if (!ok) break;
-          bool have_k = false;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (w >> x & 1) {
-              unsigned& np = x ? np1 : np0;
-              ok = mbar_wait(&b_p[x], np & 1, abort, a.dbg, 205u, (unsigned)ii);
-              if (!ok) break;
-              ++np;
-              tc_fence_after();
-              bool& fresh = x ? fresh1 : fresh0;
-              const uint32_t vlo = v_lo + (uint32_t)(vat % ST) * (L::TILE >> 4);
-#pragma unroll
-              for (int ks = 0; ks < kAttTok / 16; ++ks)
-                mma_f16_ts_lo(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, vlo + ks * (2048u >> 4), hi, id_o,
-                              (!fresh || ks > 0) ? 1u : 0u);
-              fresh = false;
-              if (--(x ? left1 : left0) == 0) mma_commit(&b_o[x]);
-            }
-            if (w2 >> x & 1) {
-              if (!have_k) {
-                ok = full(kat);
-                if (!ok) break;
-                have_k = true;
-              }
-              tc_fence_after();
-              s_mma(x, kat);
-            }
-          }
-          if (!ok) break;
-          mma_commit(&b_empty[vat % ST]);
-          ++gk;
-          if (i + st.look < st.n) {
-            mma_commit(&b_empty[kat % ST]);
-            ++gk;
-            if (i + st.look == st.n - 1) mma_commit(b_qempty);
-          }
+          pass(i);
+          if (i + st.look < st.n) pass(-1);
         }
         if (!ok) break;
-        g = gk;
+        if (lane == 0) {
+          flags[2 * (k % kItemRing) + warp - 10] = found;
+          mbar_arrive(&b_look[k % kItemRing]);
+          mbar_arrive(&b_free[k % kItemRing]);
+        }
+        __syncwarp();
       }
-      // all issued MMAs complete before TMEM is released
-      mma_commit(b_drain);
-      mbar_wait_drain(b_drain, 0);
-    }
-    __syncwarp();
     }
   } else {
     // ------------------------------------------------------------ softmax
@@ -367,57 +520,58 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + X * 128, t_o = tmem + lanes + 256 + X * 128;
+    uint4* const buf = reinterpret_cast<uint4*>(smem + L::OUT + warp * 4096);
     const float c = a.c, grow = 8.f / c;
     const int row_t = row / a.G, row_g = row % a.G;
-    unsigned ns = 0, no = 0;  // S tiles and results taken
-    int g0 = 0;               // loads of the items before
-    for (int ii = i0; ii < i1; ii += istep) {
-      const AttnItem it = item(ii);
-      const Steps<TREE> st(a, it);
-      const int tx = it.t0 + (st.alt ? 0 : X * tpt);  // this tile's first token
-      const int t = tx + row_t;
+    unsigned ns = 0, no = 0, nx = 0;  // S tiles, results and exchanges so far
+    AttnItem it;
+    for (int k = 0; __all_sync(0xffffffffu, take(k, it, 209u)); ++k) {
+      const Steps<TREE> st(it);
+      const int t = it.t0 + (st.alt ? 0 : X * tpt) + row_t;
       const bool valid = row < tpt * a.G && t < it.tend;
       const bool busy = __any_sync(0xffffffffu, valid);  // warps whose rows hold nothing skip the arithmetic
-      const int draft = TREE ? (it.klen + kAttTok - 1) / kAttTok : -1;
       const int lim = valid ? att_limit(it, t) : 0;
-      const int lim0 = TREE ? it.klen : att_limit(it, tx);  // the tile's first row's
+      const bool drafts = TREE && st.j0 <= st.draft && st.draft < st.j1;
       uint32_t nodes[4] = {};
-      bool sees = lim > 0;
-      if (TREE && valid && it.j1 > draft)
-        sees = tree_mask(a.parents + (long long)(it.lb % a.batch) * a.nodes, t, nodes);
+      bool sees = TREE || lim > 0;
+      if (drafts && valid) sees = tree_mask(a.parents + (long long)(it.lb % a.batch) * a.nodes, t, nodes);
 
       float m = -INFINITY, l = 0.f;
-      uint32_t look = 0;
       int mine = 0;  // steps of this tile so far
       for (int i = 0; i < st.n; ++i) {
         if (!(st.who(i) >> X & 1)) continue;
         const int j = st.tile(i);
-        mbar_wait(&b_s[X], ns & 1, abort, a.dbg, 206u + X, (unsigned)ii);
+        mbar_wait(&b_s[X], ns & 1, abort, a.dbg, 210u + X, (unsigned)k);
         ++ns;
-        tc_fence_after();
-        const bool masked = TREE ? (j == draft || (j + 1) * kAttTok > it.klen) : (j + 1) * kAttTok > lim0;
         if (busy) {
+          tc_fence_after();
           float s[4][32];
 #pragma unroll
           for (int q = 0; q < 4; ++q) tmem_ld32(t_s + q * 32, s[q]);
           tmem_ld_wait();
-          if (masked) {
+          if (st.masked(i, X)) {
             const int cnt = lim - j * kAttTok;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              const uint32_t w = TREE && j == draft ? nodes[q] : below(cnt, q);
+              const uint32_t w = TREE && j == st.draft ? nodes[q] : below(cnt, q);
+              if (__any_sync(0xffffffffu, w != 0xffffffffu)) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) s[q][e] = (w >> e & 1u) ? s[q][e] : -INFINITY;
+                for (int e = 0; e < 32; ++e) s[q][e] = (w >> e & 1u) ? s[q][e] : -INFINITY;
+              }
             }
           }
           float mt[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            mt[q] = s[q][0];
+            float x = fmaxf(s[q][0], s[q][1]), y = fmaxf(s[q][2], s[q][3]);
 #pragma unroll
-            for (int e = 1; e < 32; ++e) mt[q] = fmaxf(mt[q], s[q][e]);
+            for (int e = 4; e < 32; e += 4) {
+              x = max3(x, s[q][e], s[q][e + 1]);
+              y = max3(y, s[q][e + 2], s[q][e + 3]);
+            }
+            mt[q] = fmaxf(x, y);
           }
-          const float mx = fmaxf(fmaxf(mt[0], mt[1]), fmaxf(mt[2], mt[3]));
+          const float mx = fmaxf(max3(mt[0], mt[1], mt[2]), mt[3]);
           const bool up = mx > m + grow;
           if (mine == 0) {
             m = mx;
@@ -439,71 +593,67 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             }
           }
           const float mc = m == -INFINITY ? 0.f : m * c;
-          float lq[4];
+          const uint64_t c2 = pair2(c, c), mc2 = pair2(-mc, -mc);
+          uint64_t sum[2] = {0, 0};  // pairs of 0.f
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             uint32_t r[16];
-            float l0 = 0.f, l1 = 0.f;
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float p0 = ex2(fmaf(s[q][e], c, -mc)), p1 = ex2(fmaf(s[q][e + 1], c, -mc));
-              l0 += p0;
-              l1 += p1;
+              const float2 x = unpair2(fma2(pair2(s[q][e], s[q][e + 1]), c2, mc2));
+              const float p0 = ex2(x.x), p1 = ex2(x.y);
+              sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair2(p0, p1));
               r[e / 2] = T::pack(p0, p1);
             }
-            lq[q] = l0 + l1;
             tmem_st16(t_s + q * 16, r);
+            if (q & 1) {
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&b_p[2 * X + q / 2]);
+            }
           }
-          l += (lq[0] + lq[1]) + (lq[2] + lq[3]);
-          tmem_st_wait();
+          const float2 z = unpair2(add2(sum[0], sum[1]));
+          l += z.x + z.y;
+        } else if (lane == 0) {
+          mbar_arrive(&b_p[2 * X]);
+          mbar_arrive(&b_p[2 * X + 1]);
         }
-        if (masked) {
-          const int at = g0 + st.v_at(i);
-          mbar_wait(&b_full[at % ST], (at / ST) & 1, abort, a.dbg, 208u + X, (unsigned)ii);
-          const uint4* vt = reinterpret_cast<const uint4*>(smem + L::RING + (at % ST) * L::TILE) + row;
-#pragma unroll 4
-          for (int e = 0; e < L::TILE / 2048; ++e) {
-            const uint4 w = vt[e * 128];
-            look = Mma<T>::look(w.x, look);
-            look = Mma<T>::look(w.y, look);
-            look = Mma<T>::look(w.z, look);
-            look = Mma<T>::look(w.w, look);
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&b_p[X]);
         ++mine;
       }
-      g0 += 2 * st.n;
 
       // ---------------------------------------------------------- the item's result
-      bool bad = (look & 0x7fff7fffu) != 0u;
       if (mine) {
-        mbar_wait(&b_o[X], no & 1, abort, a.dbg, 210u + X, (unsigned)ii);
+        mbar_wait(&b_o[X], no & 1, abort, a.dbg, 212u + X, (unsigned)k);
         ++no;
         tc_fence_after();
       }
+      mbar_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, a.dbg, 214u, (unsigned)k);
+      const int found = flags[2 * (k % kItemRing)] | flags[2 * (k % kItemRing) + 1];
+      const bool bad = st.alt ? found != 0 : (found >> X & 1) != 0;
       if (st.alt) {
-        if (mine == 0) m = -INFINITY, l = 0.f;
         xch[X * 128 + row] = make_float2(m, l);
-        bad = named_bar_or(3, 256, bad);
-      } else {
-        bad = named_bar_or(1 + X, 128, bad);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b_x[0]);
+        mbar_wait(&b_x[0], nx & 1, abort, a.dbg, 215u, (unsigned)k);
+        tc_fence_after();
       }
-      RowOut<T, D> ro;
-      const int head = it.h * a.G + row_g;
       auto place = [&](int tok, int hd, int r) {
-        RowOut<T, D> x;
-        x.out = reinterpret_cast<uint32_t*>(a.out + it.lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h);
+        RowOut x;
         x.lse = a.lse ? a.lse + (long long)tok * a.kvh * a.G + hd : nullptr;
-        x.part = it.slot >= 0 ? a.part + ((long long)it.slot * a.prows + r) * D : nullptr;
-        x.part_ml = it.slot >= 0 ? a.part_ml + ((long long)it.slot * a.prows + r) : nullptr;
+        if (it.slot >= 0) {
+          x.out = reinterpret_cast<uint8_t*>(a.part + ((long long)it.slot * a.prows + r) * D);
+          x.part_ml = a.part_ml + ((long long)it.slot * a.prows + r);
+        } else {
+          x.out = reinterpret_cast<uint8_t*>(a.out + it.lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h);
+          x.part_ml = nullptr;
+        }
         return x;
       };
-      const int prow = (st.alt ? 0 : X * 128) + row;
-      ro = place(t, head, prow);
-      ro.sees = TREE && it.j1 <= draft ? true : sees;
+      const int head = it.h * a.G + row_g, prow = (st.alt ? 0 : X * 128) + row;
+      RowOut ro = place(t, head, prow);
+      ro.sees = sees;
       if (bad) {
         // a value that is not finite in a tile that is masked in part: this tile's rows anew
         // (of two results over the same rows, by the first warpgroup)
@@ -515,20 +665,20 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             uint32_t w[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) w[q] = __shfl_sync(0xffffffffu, nodes[q], rr);
-            const int from = it.j0 * kAttTok, to = min(see, it.j1 * kAttTok);
-            RowOut<T, D> x = place(tok, hd, __shfl_sync(0xffffffffu, prow, rr));
-            x.sees = __shfl_sync(0xffffffffu, (int)ro.sees, rr);
+            RowOut x = place(tok, hd, __shfl_sync(0xffffffffu, prow, rr));
+            x.sees = __shfl_sync(0xffffffffu, (int)sees, rr);
+            const int from = it.j0 * kAttTok, to = x.sees ? min(see, it.j1 * kAttTok) : from;
             float o[D / 32], mm, ll;
             const long long dr = (long long)it.y * a.nodes * D;
             attend_row<T, D>(a, a.q + it.lb * a.q_lb + (long long)tok * a.q_t + hd * a.q_h,
                              a.k + it.k0 * a.k_t + it.y * a.k_y, a.v + it.k0 * a.v_t + it.y * a.v_y, a.kd + dr, a.vd + dr,
-                             from, x.sees ? to : from, TREE && it.j1 > draft && x.sees ? w : nullptr, mm, ll, o);
+                             from, to, drafts && x.sees ? w : nullptr, mm, ll, o);
             if (lane == 0) x.stats(a, mm, ll);
             const float inv = x.sees ? 1.f / ll : 0.f;
 #pragma unroll
             for (int e = 0; e < D / 64; ++e) {
-              if (x.part) reinterpret_cast<float2*>(x.part)[lane * (D / 64) + e] = make_float2(o[2 * e], o[2 * e + 1]);
-              else x.out[lane * (D / 64) + e] = T::pack(o[2 * e] * inv, o[2 * e + 1] * inv);
+              if (x.part_ml) reinterpret_cast<float2*>(x.out)[lane * (D / 64) + e] = make_float2(o[2 * e], o[2 * e + 1]);
+              else reinterpret_cast<uint32_t*>(x.out)[lane * (D / 64) + e] = T::pack(o[2 * e] * inv, o[2 * e + 1] * inv);
             }
           }
         }
@@ -545,9 +695,10 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           l = l * f + y.y * fy;
           m = mm;
         }
-        const float inv = ro.part ? 1.f : ro.sees ? 1.f / l : 0.f;
+        const float inv = ro.part_ml ? 1.f : sees ? 1.f / l : 0.f;
         const int d0 = st.alt ? X * (D / 2) : 0, d1 = st.alt ? d0 + D / 2 : D;
         if (valid && (!st.alt || X == 0)) ro.stats(a, m, l);
+#pragma unroll 1
         for (int d = d0; d < d1; d += 32) {
           float o[32];
           if (mine) {
@@ -557,40 +708,40 @@ __global__ void __launch_bounds__(kAttThreads, 1)
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 0.f;
           }
-          if (st.alt) {
+          if (other) {
             float z[32];
-            if (other) {
-              tmem_ld32(tmem + lanes + 256 + (X ^ 1) * 128 + d, z);
-              tmem_ld_wait();
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) z[e] = 0.f;
-            }
+            tmem_ld32(tmem + lanes + 256 + (X ^ 1) * 128 + d, z);
+            tmem_ld_wait();
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = fmaf(z[e], fy, o[e] * f);
           }
-          if (!ro.sees) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
-          }
-          if (valid) {
-            if (ro.part) {
+          for (int e = 0; e < 32; ++e) o[e] = sees ? o[e] * inv : 0.f;
+          if (ro.part_ml) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 4)
-                *reinterpret_cast<float4*>(ro.part + d + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-            } else {
+            for (int e = 0; e < 8; ++e)
+              buf[lane * 8 + (e ^ (lane & 7))] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                                                            __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+            flush_rows<8>(buf, ro.out + d * 4, valid);
+          } else {
 #pragma unroll
-              for (int e = 0; e < 32; e += 8)
-                *reinterpret_cast<uint4*>(ro.out + (d + e) / 2) =
-                    make_uint4(T::pack(o[e] * inv, o[e + 1] * inv), T::pack(o[e + 2] * inv, o[e + 3] * inv),
-                               T::pack(o[e + 4] * inv, o[e + 5] * inv), T::pack(o[e + 6] * inv, o[e + 7] * inv));
-            }
+            for (int e = 0; e < 4; ++e)
+              buf[lane * 4 + (e ^ (lane & 3))] =
+                  make_uint4(T::pack(o[8 * e], o[8 * e + 1]), T::pack(o[8 * e + 2], o[8 * e + 3]),
+                             T::pack(o[8 * e + 4], o[8 * e + 5]), T::pack(o[8 * e + 6], o[8 * e + 7]));
+            flush_rows<4>(buf, ro.out + d * 2, valid);
           }
         }
       }
       tc_fence_before();
-      // the other warpgroup has read this one's O and statistics before they are written again
-      if (st.alt) named_bar(3, 256);
+      __syncwarp();
+      if (st.alt) {
+        // the other warpgroup has read this one's O and statistics before they are written again
+        if (lane == 0) mbar_arrive(&b_x[1]);
+        mbar_wait(&b_x[1], nx & 1, abort, a.dbg, 216u, (unsigned)k);
+        ++nx;
+      }
+      if (lane == 0) mbar_arrive(&b_free[k % kItemRing]);
     }
   }
   __syncthreads();
@@ -601,9 +752,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   if (threadIdx.x == 0 && *abort) atomicOr(a.status, kStatusTimeout);
 }
 
-// Joins the partial results of work items that share their query rows, in order: a warp per
-// row. Prompts: `merges` lists each group's first item and its parts; trees: nsplit
-// consecutive items each.
+// Joins the partial results of the parts of one item, in order: a warp per row. Prompts: `merges`
+// lists each item's first part and their number; trees: merge i belongs to the boundary between
+// CTAs i and i + 1, if that is the first one within its item.
 template <class T, int D, bool TREE>
 __global__ void __launch_bounds__(256) merge_kernel(const AttnArgs a) {
   grid_dep_wait();
@@ -613,33 +764,41 @@ __global__ void __launch_bounds__(256) merge_kernel(const AttnArgs a) {
     const int gi = (int)(u / a.prows), r = (int)(u % a.prows);
     AttnItem it;
     int parts;
+    int slot;  // of the first part; the others': every one (prompts), or every second from 2 (b + 1)
     if constexpr (TREE) {
-      it = tree_item(a, gi * a.nsplit);
-      parts = a.nsplit;
+      const long long cut = tree_from(a, gi + 1), i0 = cut / a.tiles * a.tiles;
+      if (cut == i0 || tree_from(a, gi) > i0) continue;
+      it = tree_item(a, gi, i0, i0 + a.tiles);
+      parts = 2;
+      while (tree_from(a, gi + parts) < i0 + a.tiles) ++parts;
+      // (a part that starts at its item's start and its CTA's is that CTA's second all the same)
+      slot = 2 * gi + 1;
     } else {
       const int2 mg = __ldg(a.merges + gi);
       it = load_item(a, mg.x);
       parts = mg.y;
+      slot = it.slot;
     }
+    auto place = [&](int s) { return (long long)(TREE && s ? 2 * (gi + s) : slot + s) * a.prows; };
     // rows of tile A, then of tile B
     const int x = r / 128, rr = r % 128, t = it.t0 + x * tpt + rr / a.G;
     if (rr >= tpt * a.G || t >= it.tend) continue;
-    const float2* ml = a.part_ml + (long long)it.slot * a.prows + r;
-    const float* part = a.part + ((long long)it.slot * a.prows + r) * D;
+    const float2* ml = a.part_ml + r;
+    const float* part = a.part + (long long)r * D;
     float m = -INFINITY, l = 0.f;
     bool sees = true;
     for (int s = 0; s < parts; ++s) {
-      const float2 v = ml[(long long)s * a.prows];
+      const float2 v = ml[place(s)];
       m = fmaxf(m, v.x);
       sees = sees && !(v.y < 0.f);
     }
     float o[D / 32] = {};
     for (int s = 0; s < parts && sees; ++s) {
-      const float2 v = ml[(long long)s * a.prows];
+      const float2 v = ml[place(s)];
       if (v.x == -INFINITY && v.y == 0.f) continue;
       const float f = v.x == -INFINITY ? 1.f : ex2((v.x - m) * a.c);
       l = fmaf(f, v.y, l);
-      const float* p = part + (long long)s * a.prows * D + lane * (D / 32);
+      const float* p = part + place(s) * D + lane * (D / 32);
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) o[e] = fmaf(f, p[e], o[e]);
     }

@@ -1048,7 +1048,7 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   a.parents = parents;
   a.status = p.status;
   a.dbg = p.dbg;
-  const long long slots = dc::tree_plan(&a, p.d, h->num_sms);
+  const long long slots = dc::tree_plan(&a, h->num_sms);
   if (slots) {
     // the partial results of rows in parts: kept with the handle, and made larger when a call needs more
     const size_t rows = (size_t)slots * a.prows;

@@ -122,6 +122,10 @@ Division plan_items(const int* q_lens, const int* k_lens, int n, int kvh, int G,
         it.j1 = (att_limit(it, std::min(it.tend, it.t0 + 2 * tpt) - 1) + kAttTok - 1) / kAttTok;
         it.slot = -1;
         it.alt = it.tend - it.t0 <= tpt;
+        it.lowA = att_limit(it, it.t0);
+        it.lowB = it.alt ? it.lowA : att_limit(it, it.t0 + tpt);
+        it.eA = it.alt ? it.j1 : (att_limit(it, it.t0 + tpt - 1) + kAttTok - 1) / kAttTok;
+        it.eB = it.j1;
         whole.push_back(it);
         total += item_cost(it);
       }

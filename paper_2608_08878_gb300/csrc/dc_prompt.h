@@ -21,9 +21,9 @@ bool att_map_kv(CUtensorMap* m, bool bf16, const void* base, int D, long long ys
                 long long t_stride);
 
 // Attention of drafted trees over the rows of a cache (AttnArgs' tree fields), D 64 or
-// 128, in a.nsplit parts of each row. tree_plan sets a.pairs, a.nsplit, a.prows, a.n_items and
-// a.n_merges, and returns the partial results' slots; launch_tree needs a.part and a.part_ml for them.
-long long tree_plan(AttnArgs* a, int D, int num_sms);
+// 128. tree_plan sets how the work is divided, and returns the partial results' slots;
+// launch_tree needs a.part and a.part_ml for them.
+long long tree_plan(AttnArgs* a, int num_sms);
 // `tokens`: the row stride in slots. *why on a map that the driver rejects.
 cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, int num_sms, cudaStream_t s, const char** why);
 

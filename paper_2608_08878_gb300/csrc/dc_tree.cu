@@ -6,26 +6,22 @@
 
 namespace dc {
 
-long long tree_plan(AttnArgs* a, int D, int num_sms) {
+long long tree_plan(AttnArgs* a, int num_sms) {
   const int tpt = kAttRows / a->G;
   a->pairs = (a->nodes + 2 * tpt - 1) / (2 * tpt);
   a->prows = a->nodes <= tpt ? a->nodes * a->G : 256;
-  const long long items = (long long)a->rows * a->pairs;
-  const int tiles = (a->n + kAttTok - 1) / kAttTok + 1;
-  // Parts of a row: as few as fill the SMs evenly. In units of a key tile's two products: a
-  // part costs its tiles (twice with two tiles of queries) and 5 for its start and end, and the
-  // merge of parts 5 more.
-  const double unit = a->nodes <= tpt ? 1.0 : 2.0;
-  double best = 0;
-  a->nsplit = 1;
-  for (int ns = 1; ns <= std::min(tiles, 64); ++ns) {
-    const double rounds = (double)((items * ns + num_sms - 1) / num_sms);
-    const double cost = rounds * ((tiles + ns - 1) / ns * unit + 5.0) + (ns > 1 ? 5.0 : 0.0);
-    if (ns == 1 || cost < best) best = cost, a->nsplit = ns;
-  }
-  a->n_items = (int)(items * a->nsplit);
-  a->n_merges = a->nsplit > 1 ? (int)items : 0;
-  return a->nsplit > 1 ? items * a->nsplit : 0;
+  a->n_items = a->rows * a->pairs;
+  a->tiles = (a->n + kAttTok - 1) / kAttTok + 1;
+  const long long total = (long long)a->n_items * a->tiles;
+  // CTAs: every SM an equal share of all key tiles, but at least 2 tiles; or, of few items,
+  // one each, where the items are so short that parts would not pay for the merge (about 6 tiles).
+  int grid = (int)std::min<long long>(num_sms, std::max<long long>(1, total / 2));
+  if (a->n_items <= num_sms && (a->tiles <= 8 || a->n_items == num_sms)) grid = a->n_items;
+  a->grid = grid;
+  bool cut = false;
+  for (int b = 1; b < grid && !cut; ++b) cut = tree_from(*a, b) % a->tiles != 0;
+  a->n_merges = cut ? grid - 1 : 0;
+  return cut ? 2ll * grid : 0;
 }
 
 cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, int num_sms, cudaStream_t s, const char** why) {
@@ -39,9 +35,8 @@ cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, int num_sms,
     *why = "cuTensorMapEncodeTiled rejected the layout";
     return cudaErrorInvalidValue;
   }
-  const int grid = std::min(a.n_items, num_sms);
-  return D == 128 ? launch_attend<TypeBf16, 128, true>(m, a, grid, num_sms, s)
-                  : launch_attend<TypeBf16, 64, true>(m, a, grid, num_sms, s);
+  return D == 128 ? launch_attend<TypeBf16, 128, true>(m, a, a.grid, num_sms, s)
+                  : launch_attend<TypeBf16, 64, true>(m, a, a.grid, num_sms, s);
 }
 
 }  // namespace dc
