@@ -62,10 +62,10 @@ struct AttnItem {
 };
 constexpr int kSeesAll = 1 << 30;
 
+// (t and off stay below 2^29, so the sum fits)
 __host__ __device__ inline int att_limit(const AttnItem& it, int t) {
-  if (it.off == kSeesAll) return it.klen;
-  const long long x = (long long)t + it.off;
-  return x < 0 ? 0 : x < it.klen ? (int)x : it.klen;
+  const int x = t + it.off;
+  return x < 0 ? 0 : x < it.klen ? x : it.klen;
 }
 
 struct TypeBf16 {

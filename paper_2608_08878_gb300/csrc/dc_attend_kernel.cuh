@@ -33,8 +33,8 @@
 // is released, and a tile of rows that meets such a value is recomputed by attend_row, which
 // reads only what a row sees.
 //
-// Results go through shared memory, 32 dims of a warp's 32 rows at a time, so that each row's 64
-// bytes leave together (a thread writing its own row cost 5000 to 7000 cycles an item).
+// Results go through shared memory, 128 bytes of each of a warp's 32 rows at a time, so that they
+// leave together (a thread writing its own row cost 5000 to 7000 cycles an item).
 //
 // Barriers: every wait is bounded, and the roles meet at mbarriers only. A wait that gives up
 // sets *abort; every warp then leaves its loop, the producer and the issuer wait for what they
@@ -111,42 +111,30 @@ __device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int b, long lon
   return it;
 }
 
-// An item's steps: key tile of step i, and which of A (1) and B (2) take it.
+// An item's steps: key tile of step i, and which of A (1) and B (2) take it: one each in turn, or
+// both from their first step on.
 template <bool TREE>
 struct Steps {
-  int n, j0, j1, eA, eB, lowA, lowB, alt, look, draft;
+  int n, j0, j1, alt, look, skipA, skipB, lowA, lowB, draft;
   __device__ __forceinline__ Steps(const AttnItem& it)
-      : n(it.j1 - it.j0), j0(it.j0), j1(it.j1), eA(it.eA), eB(it.eB), lowA(it.lowA), lowB(it.lowB), alt(it.alt),
-        look(it.alt ? 2 : 1), draft(TREE ? (it.klen + kAttTok - 1) / kAttTok : -1) {}
+      : n(it.j1 - it.j0), j0(it.j0), j1(it.j1), alt(it.alt), look(it.alt ? 2 : 1), skipA(max(0, it.j1 - it.eA)),
+        skipB(max(0, it.j1 - it.eB)), lowA(it.lowA), lowB(it.lowB),
+        draft(TREE ? (it.klen + kAttTok - 1) / kAttTok : -1) {}
   // the tiles that may be masked come first in prompts, last in trees
   __device__ __forceinline__ int tile(int i) const { return TREE ? j0 + i : j1 - 1 - i; }
-  __device__ __forceinline__ int who(int i) const {
-    if (i >= n) return 0;
-    if (alt) return 1 << (i & 1);
-    if (TREE) return 3;
-    const int j = tile(i);
-    return (j < eA ? 1 : 0) | (j < eB ? 2 : 0);
-  }
   // whether some row of tile A (x = 0) or B must not see some key of step i's tile
   __device__ __forceinline__ bool masked(int i, int x) const {
     const int j = tile(i);
     return (TREE && j == draft) || (j + 1) * kAttTok > (x ? lowB : lowA);
   }
-  // of those that take the step
+  // which of those that take the step
   __device__ __forceinline__ int masked(int i) const {
-    const int w = who(i);
+    const int w = alt ? 1 << (i & 1) : (i >= skipA ? 1 : 0) | (i >= skipB ? 2 : 0);
     return (w & 1 && masked(i, 0) ? 1 : 0) | (w & 2 && masked(i, 1) ? 2 : 0);
   }
   // steps of A (x = 0) or B
-  __device__ __forceinline__ int count(int x) const {
-    return alt ? (n + 1 - x) / 2 : max(0, min(x ? eB : eA, j1) - j0);
-  }
+  __device__ __forceinline__ int count(int x) const { return alt ? (n + 1 - x) / 2 : max(0, n - (x ? skipB : skipA)); }
 };
-
-__device__ __forceinline__ uint32_t below(int count, int word) {
-  const int c = count - 32 * word;
-  return c >= 32 ? 0xffffffffu : c <= 0 ? 0u : (1u << c) - 1u;
-}
 
 template <class T>
 struct Mma;
@@ -196,6 +184,15 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
+// A place in the ring of stages, and how often the ring has come round (the phase).
+template <int ST>
+struct Place {
+  uint32_t s = 0, phase = 0;
+  __device__ __forceinline__ void operator++() {
+    if (++s == ST) s = 0, phase ^= 1u;
+  }
+};
+
 // Where one row's result goes: o / l and lse, or, of a part of the keys, o, m and l.
 struct RowOut {
   uint8_t* out;    // the row's output, or its place in the partial results
@@ -208,20 +205,21 @@ struct RowOut {
   }
 };
 
-// A warp's 32 rows of C 16-byte chunks from its buffer (row r's chunk e at r * C + (e ^ (r % C)))
-// to `to` of each row, where `on`.
-template <int C>
-__device__ __forceinline__ void flush_rows(const uint4* buf, uint8_t* to, bool on) {
-  const int lane = threadIdx.x & 31, e = lane % C;
+// A warp's 32 rows of 8 16-byte chunks from its buffer (row r's chunk e at r * 8 + (e ^ (r % 8))) to
+// global memory: lane writes chunk lane % 8 of rows 4 i + lane / 8, to[i] + at, where on.
+__device__ __forceinline__ void flush_rows(const uint4* buf, uint8_t* const (&to)[8], uint32_t on, int at) {
+  const int lane = threadIdx.x & 31, e = lane & 7;
   __syncwarp();
+  uint4 v[8];
 #pragma unroll
-  for (int i = 0; i < C; ++i) {
-    const int r = i * (32 / C) + lane / C;
-    const uint4 v = buf[r * C + (e ^ (r % C))];
-    uint8_t* p = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), r));
-    if (__shfl_sync(0xffffffffu, (int)on, r)) *reinterpret_cast<uint4*>(p + e * 16) = v;
+  for (int i = 0; i < 8; ++i) {
+    const int r = i * 4 + lane / 8;
+    v[i] = buf[r * 8 + (e ^ (r & 7))];
   }
   __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (on >> (i * 4 + lane / 8) & 1u) *reinterpret_cast<uint4*>(to[i] + at) = v[i];
 }
 
 template <class T, int D, bool TREE>
@@ -283,14 +281,10 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   grid_dep_launch();  // the partial results' merge, if any, may get ready
   const int tpt = kAttRows / a.G;
 
-  // The published item number k, or false: no more, or a wait gave up.
-  auto take = [&](int k, AttnItem& it, unsigned site) {
+  // Waits for published item number k; false: no more, or the wait gave up.
+  auto ready = [&](int k, unsigned site) {
     const int e = k % kItemRing;
-    if (!mbar_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k)) return false;
-    const int4* p = reinterpret_cast<const int4*>(ring + e);
-    const int4 x = p[0], y = p[1], z = p[2], w = p[3];
-    it = AttnItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w, w.x, w.y, w.z, w.w};
-    return it.y >= 0;
+    return mbar_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k) && ring[e].y >= 0;
   };
 
   if (warp >= 8) {
@@ -371,23 +365,21 @@ __global__ void __launch_bounds__(kAttThreads, 1)
                        v_lo = sdesc_lo(smem_u32(smem + L::RING), 16384);
         constexpr uint32_t hi = sdesc_hi(1024, 2);
         constexpr uint32_t id_s = Mma<T>::id(128, 0), id_o = Mma<T>::id(D, 1);
-        int g = 0, items = 0;
-        unsigned np0 = 0, np1 = 0;  // P tiles taken of A and B
+        Place<ST> g;
+        uint32_t items = 0, np[2] = {0, 0};  // query tiles and P tiles taken, modulo 2
         bool ok = true;
-        AttnItem it;
-        for (int k = 0; ok && take(k, it, 203u); ++k) {
-          const Steps<TREE> st(it);
+        for (int k = 0; ok && ready(k, 203u); ++k) {
+          const Steps<TREE> st(ring[k % kItemRing]);
           if (st.n == 0) {
             mbar_arrive(&b_free[k % kItemRing]);
             continue;
           }
-          ok = mbar_wait(b_qfull, items & 1, abort, a.dbg, 204u, (unsigned)k);
+          ok = mbar_wait(b_qfull, items, abort, a.dbg, 204u, (unsigned)k);
           if (!ok) break;
-          ++items;
-          auto full = [&](int at) { return mbar_wait(&b_full[at % ST], (at / ST) & 1, abort, a.dbg, 205u, (unsigned)at); };
-          auto s_mma = [&](int x, int at) {
-            const uint32_t klo = k_lo + (uint32_t)(at % ST) * (L::TILE >> 4);
-            const uint32_t qlo = q_lo + (st.alt ? 0u : (uint32_t)x * (L::TILE >> 4));
+          items ^= 1u;
+          auto full = [&](const Place<ST>& p) { return mbar_wait(&b_full[p.s], p.phase, abort, a.dbg, 205u, (unsigned)k); };
+          auto s_mma = [&](int x, uint32_t qlo, uint32_t stage) {
+            const uint32_t klo = k_lo + stage * (L::TILE >> 4);
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
               const uint32_t off = ((uint32_t)(ks >> 2) * 16384u + (uint32_t)(ks & 3) * 32u) >> 4;
@@ -395,64 +387,87 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             }
             mma_commit(&b_s[x]);
           };
-          auto release = [&](int at) { mma_commit(&b_empty[at % ST]); };
-          for (int i = 0; i < st.look && i < st.n; ++i) {
+          auto o_mma = [&](int x, uint32_t stage, uint32_t fresh) {
+            const uint32_t vlo = v_lo + stage * (L::TILE >> 4);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (!mbar_wait(&b_p[2 * x + h], np[x], abort, a.dbg, 206u, (unsigned)k)) return false;
+              tc_fence_after();
+#pragma unroll
+              for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
+                mma_f16_ts_lo(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, vlo + ks * (2048u >> 4), hi, id_o,
+                              ks > 0 ? 1u : fresh ^ 1u);
+            }
+            np[x] ^= 1u;
+            return true;
+          };
+          const int n = st.n;
+          if (st.alt) {
+            // A: steps 0, 2, ..., B: 1, 3, ...; S of a step goes out behind O of the one two before
+            for (int i = 0; i < 2 && i < n; ++i) {
+              ok = ok && full(g);
+              if (!ok) break;
+              tc_fence_after();
+              if (i == 0) s_mma(0, q_lo, g.s);
+              else s_mma(1, q_lo, g.s);
+              mma_commit(&b_empty[g.s]);
+              ++g;
+            }
+            if (!ok) break;
+            if (n <= 2) mma_commit(b_qempty);
+            auto step = [&](int x, int i) {
+              if (!full(g) || !o_mma(x, g.s, i < 2)) return false;
+              mma_commit(&b_empty[g.s]);
+              if (i >= n - 2) mma_commit(&b_o[x]);
+              ++g;
+              if (i + 2 < n) {
+                if (!full(g)) return false;
+                tc_fence_after();
+                s_mma(x, q_lo, g.s);
+                mma_commit(&b_empty[g.s]);
+                ++g;
+                if (i + 3 == n) mma_commit(b_qempty);
+              }
+              return true;
+            };
+            for (int i = 0; i < n && ok; i += 2) {
+              ok = step(0, i);
+              if (ok && i + 1 < n) ok = step(1, i + 1);
+            }
+          } else {
+            const uint32_t qb = q_lo + (L::TILE >> 4);
             ok = full(g);
             if (!ok) break;
             tc_fence_after();
-            const int w = st.who(i);
-            if (w & 1) s_mma(0, g);
-            if (w & 2) s_mma(1, g);
-            release(g);
+            if (st.skipA == 0) s_mma(0, q_lo, g.s);
+            if (st.skipB == 0) s_mma(1, qb, g.s);
+            mma_commit(&b_empty[g.s]);
+            if (n == 1) mma_commit(b_qempty);
             ++g;
-          }
-          if (!ok) break;
-          if (st.look >= st.n) mma_commit(b_qempty);
-          int left0 = st.count(0), left1 = st.count(1);  // steps to come
-          bool fresh0 = true, fresh1 = true;
-          for (int i = 0; i < st.n; ++i) {
-            const int w = st.who(i), w2 = st.who(i + st.look), vat = g, kat = g + 1;
-            ok = full(vat);
-            if (!ok) break;
-            bool have_k = false;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if (w >> x & 1) {
-                unsigned& np = x ? np1 : np0;
-                bool& fresh = x ? fresh1 : fresh0;
-                const uint32_t vlo = v_lo + (uint32_t)(vat % ST) * (L::TILE >> 4);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  ok = ok && mbar_wait(&b_p[2 * x + h], np & 1, abort, a.dbg, 206u, (unsigned)k);
-                  if (!ok) break;
-                  tc_fence_after();
-#pragma unroll
-                  for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
-                    mma_f16_ts_lo(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, vlo + ks * (2048u >> 4), hi, id_o,
-                                  (!fresh || ks > 0) ? 1u : 0u);
-                }
-                if (!ok) break;
-                ++np;
-                fresh = false;
-                if (--(x ? left1 : left0) == 0) mma_commit(&b_o[x]);
-              }
-              if (w2 >> x & 1) {
-                if (!have_k) {
-                  ok = full(kat);
-                  if (!ok) break;
-                  have_k = true;
-                }
-                tc_fence_after();
-                s_mma(x, kat);
-              }
-            }
-            if (!ok) break;
-            release(vat);
-            ++g;
-            if (i + st.look < st.n) {
-              release(kat);
+            for (int i = 0; i < n; ++i) {
+              const Place<ST> gv = g;
               ++g;
-              if (i + st.look == st.n - 1) mma_commit(b_qempty);
+              const bool more = i + 1 < n;
+              ok = full(gv) && (!more || full(g));
+              if (!ok) break;
+              if (i >= st.skipA) {
+                ok = o_mma(0, gv.s, i == st.skipA);
+                if (!ok) break;
+                if (!more) mma_commit(&b_o[0]);
+              }
+              if (more && i + 1 >= st.skipA) s_mma(0, q_lo, g.s);
+              if (i >= st.skipB) {
+                ok = o_mma(1, gv.s, i == st.skipB);
+                if (!ok) break;
+                if (!more) mma_commit(&b_o[1]);
+              }
+              if (more && i + 1 >= st.skipB) s_mma(1, qb, g.s);
+              mma_commit(&b_empty[gv.s]);
+              if (more) {
+                mma_commit(&b_empty[g.s]);
+                if (i + 2 == n) mma_commit(b_qempty);
+                ++g;
+              }
             }
           }
           if (ok) mbar_arrive(&b_free[k % kItemRing]);
@@ -466,14 +481,13 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       // ---------------------------------------------------------- values of partly masked tiles
       // (These warps wait for and release every load, so that a stage's phase cannot pass them by,
       // nor they it: a wait for a parity is sound only one phase away.)
-      int g = 0;
-      AttnItem it;
-      for (int k = 0; __all_sync(0xffffffffu, take(k, it, 207u)); ++k) {
-        const Steps<TREE> st(it);
+      Place<ST> g;
+      for (int k = 0; __all_sync(0xffffffffu, ready(k, 207u)); ++k) {
+        const Steps<TREE> st(ring[k % kItemRing]);
         int found = 0;
         bool ok = true;
         auto pass = [&](int i) {  // i >= 0: V of step i, else some K
-          ok = __all_sync(0xffffffffu, ok && mbar_wait(&b_full[g % ST], (g / ST) & 1, abort, a.dbg, 208u, (unsigned)g));
+          ok = __all_sync(0xffffffffu, ok && mbar_wait(&b_full[g.s], g.phase, abort, a.dbg, 208u, (unsigned)k));
           const int mk = ok && i >= 0 ? st.masked(i) : 0;
           if (mk) {
             // the keys that some row must not see
@@ -483,7 +497,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             uint32_t acc[4] = {};
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
-              const uint4* vt = reinterpret_cast<const uint4*>(smem + L::RING + (g % ST) * L::TILE + c * 16384);
+              const uint4* vt = reinterpret_cast<const uint4*>(smem + L::RING + g.s * L::TILE + c * 16384);
 #pragma unroll 4
               for (int e = lo * 8 + (warp - 10) * 32 + lane; e < hi * 8; e += 64) {
                 const uint4 w = vt[e];
@@ -496,7 +510,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             if (__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7fff7fffu) != 0u)) found |= mk;
           }
           __syncwarp();
-          if (ok && lane == 0) mbar_arrive(&b_empty[g % ST]);
+          if (ok && lane == 0) mbar_arrive(&b_empty[g.s]);
           ++g;
         };
         for (int i = 0; i < st.look && i < st.n; ++i) pass(-1);
@@ -523,9 +537,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     uint4* const buf = reinterpret_cast<uint4*>(smem + L::OUT + warp * 4096);
     const float c = a.c, grow = 8.f / c;
     const int row_t = row / a.G, row_g = row % a.G;
-    unsigned ns = 0, no = 0, nx = 0;  // S tiles, results and exchanges so far
-    AttnItem it;
-    for (int k = 0; __all_sync(0xffffffffu, take(k, it, 209u)); ++k) {
+    uint32_t ns = 0, no = 0, nx = 0;  // S tiles, results and exchanges so far, modulo 2
+    for (int k = 0; __all_sync(0xffffffffu, ready(k, 209u)); ++k) {
+      const AttnItem& it = ring[k % kItemRing];  // (not kept in registers through the steps)
       const Steps<TREE> st(it);
       const int t = it.t0 + (st.alt ? 0 : X * tpt) + row_t;
       const bool valid = row < tpt * a.G && t < it.tend;
@@ -537,12 +551,12 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       if (drafts && valid) sees = tree_mask(a.parents + (long long)(it.lb % a.batch) * a.nodes, t, nodes);
 
       float m = -INFINITY, l = 0.f;
-      int mine = 0;  // steps of this tile so far
-      for (int i = 0; i < st.n; ++i) {
-        if (!(st.who(i) >> X & 1)) continue;
+      const int mine = st.count(X), i0 = st.alt ? X : X ? st.skipB : st.skipA, istep = st.alt ? 2 : 1;
+#pragma unroll 1
+      for (int i = i0; i < st.n; i += istep) {
         const int j = st.tile(i);
-        mbar_wait(&b_s[X], ns & 1, abort, a.dbg, 210u + X, (unsigned)k);
-        ++ns;
+        mbar_wait(&b_s[X], ns, abort, a.dbg, 210u + X, (unsigned)k);
+        ns ^= 1u;
         if (busy) {
           tc_fence_after();
           float s[4][32];
@@ -550,13 +564,22 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           for (int q = 0; q < 4; ++q) tmem_ld32(t_s + q * 32, s[q]);
           tmem_ld_wait();
           if (st.masked(i, X)) {
-            const int cnt = lim - j * kAttTok;
+            if (TREE && j == st.draft) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const uint32_t w = TREE && j == st.draft ? nodes[q] : below(cnt, q);
-              if (__any_sync(0xffffffffu, w != 0xffffffffu)) {
+              for (int q = 0; q < 4; ++q) {
+                const uint32_t w = nodes[q];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) s[q][e] = (w >> e & 1u) ? s[q][e] : -INFINITY;
+              }
+            } else {
+              // (quarters that every row of the warp sees stay as they are)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const int cnt = lim - j * kAttTok - q * 32;
+                if (__any_sync(0xffffffffu, cnt < 32)) {
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) s[q][e] = e < cnt ? s[q][e] : -INFINITY;
+                }
               }
             }
           }
@@ -573,7 +596,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           }
           const float mx = fmaxf(max3(mt[0], mt[1], mt[2]), mt[3]);
           const bool up = mx > m + grow;
-          if (mine == 0) {
+          if (i == i0) {
             m = mx;
           } else if (__any_sync(0xffffffffu, up)) {
             const float f = up ? ex2((m - mx) * c) : 1.f;
@@ -619,13 +642,12 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           mbar_arrive(&b_p[2 * X]);
           mbar_arrive(&b_p[2 * X + 1]);
         }
-        ++mine;
       }
 
       // ---------------------------------------------------------- the item's result
       if (mine) {
-        mbar_wait(&b_o[X], no & 1, abort, a.dbg, 212u + X, (unsigned)k);
-        ++no;
+        mbar_wait(&b_o[X], no, abort, a.dbg, 212u + X, (unsigned)k);
+        no ^= 1u;
         tc_fence_after();
       }
       mbar_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, a.dbg, 214u, (unsigned)k);
@@ -636,7 +658,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&b_x[0]);
-        mbar_wait(&b_x[0], nx & 1, abort, a.dbg, 215u, (unsigned)k);
+        mbar_wait(&b_x[0], nx, abort, a.dbg, 215u, (unsigned)k);
         tc_fence_after();
       }
       auto place = [&](int tok, int hd, int r) {
@@ -698,9 +720,15 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         const float inv = ro.part_ml ? 1.f : sees ? 1.f / l : 0.f;
         const int d0 = st.alt ? X * (D / 2) : 0, d1 = st.alt ? d0 + D / 2 : D;
         if (valid && (!st.alt || X == 0)) ro.stats(a, m, l);
-#pragma unroll 1
-        for (int d = d0; d < d1; d += 32) {
-          float o[32];
+        // where this lane's share of the rows goes
+        uint8_t* to[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          to[i] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(ro.out),
+                                                         i * 4 + lane / 8)) + (lane & 7) * 16;
+        const uint32_t on = __ballot_sync(0xffffffffu, valid);
+        // 32 dims of this row's result
+        auto dims = [&](int d, float (&o)[32]) {
           if (mine) {
             tmem_ld32(t_o + d, o);
             tmem_ld_wait();
@@ -716,20 +744,36 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             for (int e = 0; e < 32; ++e) o[e] = fmaf(z[e], fy, o[e] * f);
           }
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = sees ? o[e] * inv : 0.f;
-          if (ro.part_ml) {
+          for (int e = 0; e < 32; ++e) o[e] *= inv;
+        };
+        if (it.slot >= 0) {
+#pragma unroll 1
+          for (int d = d0; d < d1; d += 32) {
+            float o[32];
+            dims(d, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               buf[lane * 8 + (e ^ (lane & 7))] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
                                                             __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
-            flush_rows<8>(buf, ro.out + d * 4, valid);
-          } else {
+            flush_rows(buf, to, on, d * 4);
+          }
+        } else {
+          // 64 dims at a time (of 32 only, each row's second half is written by no lane)
+          const uint32_t half = d1 - d0 < 64 && (lane & 4) ? 0u : on;
+#pragma unroll 1
+          for (int d = d0; d < d1; d += 64) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              buf[lane * 4 + (e ^ (lane & 3))] =
-                  make_uint4(T::pack(o[8 * e], o[8 * e + 1]), T::pack(o[8 * e + 2], o[8 * e + 3]),
-                             T::pack(o[8 * e + 4], o[8 * e + 5]), T::pack(o[8 * e + 6], o[8 * e + 7]));
-            flush_rows<4>(buf, ro.out + d * 2, valid);
+            for (int h = 0; h < 2; ++h) {
+              if (d + h * 32 >= d1) break;
+              float o[32];
+              dims(d + h * 32, o);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                buf[lane * 8 + ((h * 4 + e) ^ (lane & 7))] =
+                    make_uint4(T::pack(o[8 * e], o[8 * e + 1]), T::pack(o[8 * e + 2], o[8 * e + 3]),
+                               T::pack(o[8 * e + 4], o[8 * e + 5]), T::pack(o[8 * e + 6], o[8 * e + 7]));
+            }
+            flush_rows(buf, to, half, d * 2);
           }
         }
       }
@@ -738,8 +782,8 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       if (st.alt) {
         // the other warpgroup has read this one's O and statistics before they are written again
         if (lane == 0) mbar_arrive(&b_x[1]);
-        mbar_wait(&b_x[1], nx & 1, abort, a.dbg, 216u, (unsigned)k);
-        ++nx;
+        mbar_wait(&b_x[1], nx, abort, a.dbg, 216u, (unsigned)k);
+        nx ^= 1u;
       }
       if (lane == 0) mbar_arrive(&b_free[k % kItemRing]);
     }
