@@ -67,8 +67,8 @@ struct AttSmem {
   static constexpr int RING = 2 * TILE;
   static constexpr int OUT = RING + STAGES * TILE;  // 4 KB a softmax warp
   static constexpr int MISC = OUT + 8 * 4096;       // barriers
-  static constexpr int ITEM = MISC + 512;           // AttnItem [4]
-  static constexpr int FLAG = ITEM + kItemRing * 64;  // int [4][2]: what warps 10 and 11 found
+  static constexpr int ITEM = MISC + 512;           // Published [4]
+  static constexpr int FLAG = ITEM + kItemRing * 96;  // int [4][2]: what warps 10 and 11 found
   static constexpr int XCH = MISC + 1024;           // float2 [2][128]: m, l of both tiles
   static constexpr int BYTES = XCH + 2048;
   static_assert(BYTES <= 232448, "more shared memory than a CTA may have");
@@ -136,6 +136,13 @@ struct Steps {
   __device__ __forceinline__ int count(int x) const { return alt ? (n + 1 - x) / 2 : max(0, n - (x ? skipB : skipA)); }
 };
 
+// What the producer tells the other warps of an item.
+struct Published {
+  AttnItem it;
+  int4 of[2];  // A's and B's: first query token, first step, number of steps, lowA or lowB
+};
+static_assert(sizeof(Published) == 96, "AttSmem::ITEM");
+
 template <class T>
 struct Mma;
 template <>
@@ -176,6 +183,17 @@ __device__ __forceinline__ float2 unpair2(uint64_t x) {
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Reciprocal to 1 unit in the last place; of 0: infinity.
+__device__ __forceinline__ float rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
@@ -242,7 +260,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
            *b_look = bar + 35, *b_x = bar + 39;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::MISC + 400);
   volatile int* abort = reinterpret_cast<int*>(smem + L::MISC + 404);
-  AttnItem* ring = reinterpret_cast<AttnItem*>(smem + L::ITEM);
+  Published* ring = reinterpret_cast<Published*>(smem + L::ITEM);
   volatile int* flags = reinterpret_cast<int*>(smem + L::FLAG);
   float2* xch = reinterpret_cast<float2*>(smem + L::XCH);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -284,7 +302,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   // Waits for published item number k; false: no more, or the wait gave up.
   auto ready = [&](int k, unsigned site) {
     const int e = k % kItemRing;
-    return mbar_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k) && ring[e].y >= 0;
+    return mbar_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k) && ring[e].it.y >= 0;
   };
 
   if (warp >= 8) {
@@ -325,9 +343,11 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           p[1] = make_int4(it.tend, it.k0, it.klen, it.off);
           p[2] = make_int4(it.j0, it.j1, it.slot, it.alt);
           p[3] = make_int4(it.eA, it.eB, it.lowA, it.lowB);
+          const Steps<TREE> st(it);
+          p[4] = make_int4(it.t0, st.alt ? 0 : st.skipA, st.count(0), it.lowA);
+          p[5] = make_int4(st.alt ? it.t0 : it.t0 + tpt, st.alt ? 1 : st.skipB, st.count(1), it.lowB);
           mbar_arrive(&b_item[e]);
           if (it.y < 0) break;
-          const Steps<TREE> st(it);
           fetch();
           if (st.n == 0) continue;
           if (!mbar_wait(b_qempty, (sent & 1) ^ 1, abort, a.dbg, 201u, (unsigned)k)) break;
@@ -369,7 +389,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         uint32_t items = 0, np[2] = {0, 0};  // query tiles and P tiles taken, modulo 2
         bool ok = true;
         for (int k = 0; ok && ready(k, 203u); ++k) {
-          const Steps<TREE> st(ring[k % kItemRing]);
+          const Steps<TREE> st(ring[k % kItemRing].it);
           if (st.n == 0) {
             mbar_arrive(&b_free[k % kItemRing]);
             continue;
@@ -483,7 +503,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       // nor they it: a wait for a parity is sound only one phase away.)
       Place<ST> g;
       for (int k = 0; __all_sync(0xffffffffu, ready(k, 207u)); ++k) {
-        const Steps<TREE> st(ring[k % kItemRing]);
+        const Steps<TREE> st(ring[k % kItemRing].it);
         int found = 0;
         bool ok = true;
         auto pass = [&](int i) {  // i >= 0: V of step i, else some K
@@ -537,24 +557,26 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     uint4* const buf = reinterpret_cast<uint4*>(smem + L::OUT + warp * 4096);
     const float c = a.c, grow = 8.f / c;
     const int row_t = row / a.G, row_g = row % a.G;
-    uint32_t ns = 0, no = 0, nx = 0;  // S tiles, results and exchanges so far, modulo 2
+    uint32_t ns = 0, no = 0, oo = 0, nx = 0;  // S tiles, results (oo: the other's) and exchanges so far, modulo 2
     for (int k = 0; __all_sync(0xffffffffu, ready(k, 209u)); ++k) {
-      const AttnItem& it = ring[k % kItemRing];  // (not kept in registers through the steps)
-      const Steps<TREE> st(it);
-      const int t = it.t0 + (st.alt ? 0 : X * tpt) + row_t;
+      const AttnItem& it = ring[k % kItemRing].it;  // (not kept in registers through the steps)
+      const int4 of = ring[k % kItemRing].of[X];
+      const int alt = it.alt, steps = of.z, low = of.w, klen = it.klen;
+      const int draft = TREE ? (klen + kAttTok - 1) / kAttTok : -1;
+      const int t = of.x + row_t;
       const bool valid = row < tpt * a.G && t < it.tend;
       const bool busy = __any_sync(0xffffffffu, valid);  // warps whose rows hold nothing skip the arithmetic
       const int lim = valid ? att_limit(it, t) : 0;
-      const bool drafts = TREE && st.j0 <= st.draft && st.draft < st.j1;
+      const bool drafts = TREE && it.j0 <= draft && draft < it.j1;
       uint32_t nodes[4] = {};
       bool sees = TREE || lim > 0;
       if (drafts && valid) sees = tree_mask(a.parents + (long long)(it.lb % a.batch) * a.nodes, t, nodes);
 
       float m = -INFINITY, l = 0.f;
-      const int mine = st.count(X), i0 = st.alt ? X : X ? st.skipB : st.skipA, istep = st.alt ? 2 : 1;
+      int j = TREE ? it.j0 + of.y : it.j1 - 1 - of.y;
+      const int jstep = TREE ? alt + 1 : -1 - alt;
 #pragma unroll 1
-      for (int i = i0; i < st.n; i += istep) {
-        const int j = st.tile(i);
+      for (int i = 0; i < steps; ++i, j += jstep) {
         mbar_wait(&b_s[X], ns, abort, a.dbg, 210u + X, (unsigned)k);
         ns ^= 1u;
         if (busy) {
@@ -563,40 +585,43 @@ __global__ void __launch_bounds__(kAttThreads, 1)
 #pragma unroll
           for (int q = 0; q < 4; ++q) tmem_ld32(t_s + q * 32, s[q]);
           tmem_ld_wait();
-          if (st.masked(i, X)) {
-            if (TREE && j == st.draft) {
+          bool live = true;  // whether any row of the warp sees any of the second 64 keys
+          if ((TREE && j == draft) || (j + 1) * kAttTok > low) {
+            if (TREE && j == draft) {
+              live = __any_sync(0xffffffffu, (nodes[2] | nodes[3]) != 0u);
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 const uint32_t w = nodes[q];
+                if (q < 2 || live) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) s[q][e] = (w >> e & 1u) ? s[q][e] : -INFINITY;
+                  for (int e = 0; e < 32; ++e) s[q][e] = (w >> e & 1u) ? s[q][e] : -INFINITY;
+                }
               }
             } else {
               // (quarters that every row of the warp sees stay as they are)
+              const int cnt = lim - j * kAttTok;
+              live = __any_sync(0xffffffffu, cnt > 64);
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const int cnt = lim - j * kAttTok - q * 32;
-                if (__any_sync(0xffffffffu, cnt < 32)) {
+              for (int q = 0; q < 4; ++q)
+                if ((q < 2 || live) && __any_sync(0xffffffffu, cnt < q * 32 + 32)) {
 #pragma unroll
-                  for (int e = 0; e < 32; ++e) s[q][e] = e < cnt ? s[q][e] : -INFINITY;
+                  for (int e = 0; e < 32; ++e) s[q][e] = q * 32 + e < cnt ? s[q][e] : -INFINITY;
                 }
-              }
             }
           }
-          float mt[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          auto top = [&](int q) {
             float x = fmaxf(s[q][0], s[q][1]), y = fmaxf(s[q][2], s[q][3]);
 #pragma unroll
             for (int e = 4; e < 32; e += 4) {
               x = max3(x, s[q][e], s[q][e + 1]);
               y = max3(y, s[q][e + 2], s[q][e + 3]);
             }
-            mt[q] = fmaxf(x, y);
-          }
-          const float mx = fmaxf(max3(mt[0], mt[1], mt[2]), mt[3]);
+            return fmaxf(x, y);
+          };
+          float mx = fmaxf(top(0), top(1));
+          if (live) mx = max3(mx, top(2), top(3));
           const bool up = mx > m + grow;
-          if (i == i0) {
+          if (i == 0) {
             m = mx;
           } else if (__any_sync(0xffffffffu, up)) {
             const float f = up ? ex2((m - mx) * c) : 1.f;
@@ -604,7 +629,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
               m = mx;
               l *= f;
             }
-#pragma unroll
+#pragma unroll 1
             for (int q = 0; q < D / 32; ++q) {
               float o[32];
               tmem_ld32(t_o + q * 32, o);
@@ -619,22 +644,28 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           const uint64_t c2 = pair2(c, c), mc2 = pair2(-mc, -mc);
           uint64_t sum[2] = {0, 0};  // pairs of 0.f
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t r[16];
+          for (int h = 0; h < 2; ++h) {
+            if (h == 0 || live) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 x = unpair2(fma2(pair2(s[q][e], s[q][e + 1]), c2, mc2));
-              const float p0 = ex2(x.x), p1 = ex2(x.y);
-              sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair2(p0, p1));
-              r[e / 2] = T::pack(p0, p1);
+              for (int q = 2 * h; q < 2 * h + 2; ++q) {
+                uint32_t r[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                  const float2 x = unpair2(fma2(pair2(s[q][e], s[q][e + 1]), c2, mc2));
+                  const float p0 = ex2(x.x), p1 = ex2(x.y);
+                  sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair2(p0, p1));
+                  r[e / 2] = T::pack(p0, p1);
+                }
+                tmem_st16(t_s + q * 16, r);
+              }
+            } else {
+              const uint32_t zero[32] = {};
+              tmem_st32(t_s + 32, zero);
             }
-            tmem_st16(t_s + q * 16, r);
-            if (q & 1) {
-              tmem_st_wait();
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&b_p[2 * X + q / 2]);
-            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&b_p[2 * X + h]);
           }
           const float2 z = unpair2(add2(sum[0], sum[1]));
           l += z.x + z.y;
@@ -645,41 +676,67 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       }
 
       // ---------------------------------------------------------- the item's result
-      if (mine) {
-        mbar_wait(&b_o[X], no, abort, a.dbg, 212u + X, (unsigned)k);
-        no ^= 1u;
-        tc_fence_after();
-      }
+      // (all that does not need O goes before the wait for it)
       mbar_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, a.dbg, 214u, (unsigned)k);
       const int found = flags[2 * (k % kItemRing)] | flags[2 * (k % kItemRing) + 1];
-      const bool bad = st.alt ? found != 0 : (found >> X & 1) != 0;
-      if (st.alt) {
+      const bool bad = alt ? found != 0 : (found >> X & 1) != 0;
+      // of two results over the same rows, each warpgroup joins half the dims
+      float f = 1.f, fy = 0.f;
+      int other = 0;
+      if (alt) {
         xch[X * 128 + row] = make_float2(m, l);
-        tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&b_x[0]);
         mbar_wait(&b_x[0], nx, abort, a.dbg, 215u, (unsigned)k);
-        tc_fence_after();
+        const float2 y = xch[(X ^ 1) * 128 + row];
+        const float mm = fmaxf(m, y.x);
+        other = ring[k % kItemRing].of[X ^ 1].z;
+        f = m == -INFINITY ? 0.f : ex2((m - mm) * c);
+        fy = y.x == -INFINITY ? 0.f : ex2((y.x - mm) * c);
+        l = l * f + y.y * fy;
+        m = mm;
       }
+      const int slot = it.slot;
       auto place = [&](int tok, int hd, int r) {
         RowOut x;
         x.lse = a.lse ? a.lse + (long long)tok * a.kvh * a.G + hd : nullptr;
-        if (it.slot >= 0) {
-          x.out = reinterpret_cast<uint8_t*>(a.part + ((long long)it.slot * a.prows + r) * D);
-          x.part_ml = a.part_ml + ((long long)it.slot * a.prows + r);
+        if (slot >= 0) {
+          x.out = reinterpret_cast<uint8_t*>(a.part + ((long long)slot * a.prows + r) * D);
+          x.part_ml = a.part_ml + ((long long)slot * a.prows + r);
         } else {
           x.out = reinterpret_cast<uint8_t*>(a.out + it.lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h);
           x.part_ml = nullptr;
         }
         return x;
       };
-      const int head = it.h * a.G + row_g, prow = (st.alt ? 0 : X * 128) + row;
+      const int head = it.h * a.G + row_g, prow = (alt ? 0 : X * 128) + row;
       RowOut ro = place(t, head, prow);
       ro.sees = sees;
+      // where this lane's share of the rows goes
+      uint8_t* to[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        to[i] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(ro.out),
+                                                       i * 4 + lane / 8)) + (lane & 7) * 16;
+      const uint32_t on = __ballot_sync(0xffffffffu, valid);
+      if (!bad && valid && (!alt || X == 0)) ro.stats(a, m, l);
+      {
+        const float inv = slot >= 0 ? 1.f : sees ? rcp(l) : 0.f;
+        f *= inv;
+        fy *= inv;
+      }
+      if (steps) {
+        mbar_wait(&b_o[X], no, abort, a.dbg, 212u + X, (unsigned)k);
+        no ^= 1u;
+      }
+      // (the other's products: it has passed its earlier results, as its part of the exchange says)
+      if (other) mbar_wait(&b_o[X ^ 1], oo, abort, a.dbg, 213u, (unsigned)k);
+      oo ^= ring[k % kItemRing].of[X ^ 1].z ? 1u : 0u;
+      tc_fence_after();
       if (bad) {
         // a value that is not finite in a tile that is masked in part: this tile's rows anew
         // (of two results over the same rows, by the first warpgroup)
-        if (!(st.alt && X == 1)) {
+        if (!(alt && X == 1)) {
           for (int rr = 0; rr < 32; ++rr) {
             if (!__shfl_sync(0xffffffffu, (int)valid, rr)) continue;
             const int tok = __shfl_sync(0xffffffffu, t, rr), hd = __shfl_sync(0xffffffffu, head, rr);
@@ -705,33 +762,11 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           }
         }
       } else if (busy) {
-        // of two results over the same rows, each warpgroup joins half the dims
-        float f = 1.f, fy = 0.f;
-        bool other = false;
-        if (st.alt) {
-          const float2 y = xch[(X ^ 1) * 128 + row];
-          const float mm = fmaxf(m, y.x);
-          other = st.count(X ^ 1) > 0;
-          f = m == -INFINITY ? 0.f : ex2((m - mm) * c);
-          fy = y.x == -INFINITY ? 0.f : ex2((y.x - mm) * c);
-          l = l * f + y.y * fy;
-          m = mm;
-        }
-        const float inv = ro.part_ml ? 1.f : sees ? 1.f / l : 0.f;
-        const int d0 = st.alt ? X * (D / 2) : 0, d1 = st.alt ? d0 + D / 2 : D;
-        if (valid && (!st.alt || X == 0)) ro.stats(a, m, l);
-        // where this lane's share of the rows goes
-        uint8_t* to[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          to[i] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(ro.out),
-                                                         i * 4 + lane / 8)) + (lane & 7) * 16;
-        const uint32_t on = __ballot_sync(0xffffffffu, valid);
+        const int d0 = alt ? X * (D / 2) : 0, d1 = alt ? d0 + D / 2 : D;
         // 32 dims of this row's result
         auto dims = [&](int d, float (&o)[32]) {
-          if (mine) {
+          if (steps) {
             tmem_ld32(t_o + d, o);
-            tmem_ld_wait();
           } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 0.f;
@@ -742,11 +777,18 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             tmem_ld_wait();
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = fmaf(z[e], fy, o[e] * f);
-          }
+          } else {
+            tmem_ld_wait();
+            const uint64_t f2 = pair2(f, f);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] *= inv;
+            for (int e = 0; e < 32; e += 2) {
+              const float2 x = unpair2(mul2(pair2(o[e], o[e + 1]), f2));
+              o[e] = x.x;
+              o[e + 1] = x.y;
+            }
+          }
         };
-        if (it.slot >= 0) {
+        if (slot >= 0) {
 #pragma unroll 1
           for (int d = d0; d < d1; d += 32) {
             float o[32];
@@ -779,7 +821,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (st.alt) {
+      if (alt) {
         // the other warpgroup has read this one's O and statistics before they are written again
         if (lane == 0) mbar_arrive(&b_x[1]);
         mbar_wait(&b_x[1], nx, abort, a.dbg, 216u, (unsigned)k);
