@@ -80,9 +80,10 @@ __device__ __forceinline__ AttnItem load_item(const AttnArgs& a, int i) {
   return AttnItem{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w, w.x, w.y, w.z, w.w};
 }
 
-// Trees: the key tiles of all items (rows' pairs of query tiles, a.tiles key tiles each: the
-// cached tokens', then the drafted ones'; rows may have fewer) in one line, of which CTA b of
-// `grid` takes the b-th equal part.
+// Trees: the key tiles of all items (every row's first pair of query tiles, then every row's
+// second one, and so on: the CTAs that read a row's keys then do so at the same time) in one
+// line, a.tiles each (the cached tokens', then the drafted ones'; rows may have fewer), of which CTA
+// b of `grid` takes the b-th equal part.
 __host__ __device__ inline long long tree_from(const AttnArgs& a, int b) {
   return (long long)a.n_items * a.tiles * b / a.grid;
 }
@@ -92,10 +93,10 @@ __device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int b, long lon
   const int tpt = kAttRows / a.G, i = (int)(at / a.tiles), j0 = (int)(at - (long long)i * a.tiles);
   const int j1 = (int)(end - at < a.tiles - j0 ? j0 + (end - at) : a.tiles);
   AttnItem it;
-  it.y = i / a.pairs;
+  it.y = i % a.rows;
   it.lb = it.y / a.kvh;
   it.h = it.y % a.kvh;
-  it.t0 = i % a.pairs * 2 * tpt;
+  it.t0 = i / a.rows * 2 * tpt;
   it.tend = a.nodes;
   it.k0 = 0;
   it.klen = a.rowlen ? __ldg(a.rowlen + it.y) : a.n;
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     if (warp == 8) {
       // ---------------------------------------------------------- producer
       if (elect_one()) {
-        const uint64_t pol = TREE ? l2_evict_first_policy() : l2_evict_normal_policy();
+        const uint64_t pol = TREE && a.pairs == 1 ? l2_evict_first_policy() : l2_evict_normal_policy();
         const uint32_t qbytes = (uint32_t)(tpt * a.G) * (uint32_t)D * 2u;
         int g = 0, sent = 0;
         long long at = 0, end = 0;

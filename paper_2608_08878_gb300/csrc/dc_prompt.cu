@@ -91,23 +91,106 @@ struct dc_prompt_plan {
 namespace dc {
 namespace {
 
+// Times in us that divide the work (measured with heads of 128 dims): a key tile of an item
+// with two tiles of query rows, or with one; an item's start and end; the second kernel and the
+// bytes of partial results that it takes in a us.
+constexpr double kStepUs = 1.4, kAltStepUs = 1.0, kItemUs = 3.5, kMergeUs = 4.0, kMergeBytes = 5e6;
+
+double step_cost(const AttnItem& it) { return it.alt ? kAltStepUs : kStepUs; }
+double item_cost(const AttnItem& it) { return (it.j1 - it.j0) * step_cost(it) + kItemUs; }
+
+// Items (of one part each) or parts, those of CTA b at [first[b], first[b + 1]).
 struct Division {
-  std::vector<AttnItem> items;  // CTA by CTA
+  std::vector<AttnItem> items;
   std::vector<int> first;
-  std::vector<int2> merges;
+  std::vector<int2> merges;  // an item's first part and its parts
   int slots = 0, prows = 0;
+  double us = 0;
 };
 
-// The time of an item in halves of a key tile's products with one tile of queries: two
-// products for each tile of queries and key tile (three halves where one tile of queries leaves
-// the tensor cores waiting for keys), and its start and end.
-double item_cost(const AttnItem& it) { return (it.j1 - it.j0) * (it.alt ? 1.5 : 2.0) + 3.0; }
+// Whole items, the longest first, each to the CTA with the least to do.
+Division divide_whole(const std::vector<AttnItem>& items, int num_sms) {
+  Division d;
+  std::vector<int> order(items.size());
+  for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return item_cost(items[a]) > item_cost(items[b]); });
+  const int grid = (int)std::min<size_t>(items.size(), (size_t)num_sms);
+  std::vector<std::vector<int>> of(grid);
+  using Load = std::pair<double, int>;
+  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+  for (int b = 0; b < grid; ++b) least.push({0.0, b});
+  for (int i : order) {
+    Load x = least.top();
+    least.pop();
+    of[x.second].push_back(i);
+    x.first += item_cost(items[i]);
+    d.us = std::max(d.us, x.first);
+    least.push(x);
+  }
+  for (int b = 0; b < grid; ++b) {
+    d.first.push_back((int)d.items.size());
+    for (int i : of[b]) d.items.push_back(items[i]);
+  }
+  d.first.push_back((int)d.items.size());
+  return d;
+}
 
-Division plan_items(const int* q_lens, const int* k_lens, int n, int kvh, int G, bool causal, int num_sms) {
+// All key tiles in one line, cut into `grid` parts of equal time. A part of an item has 2 key
+// tiles at least.
+Division divide_cut(const std::vector<AttnItem>& items, int grid, int G, int D) {
+  Division d;
+  double total = grid * kItemUs;  // (each cut starts an item once more)
+  for (const AttnItem& it : items) total += item_cost(it);
+  // (what a CTA leaves of its share goes to the next one)
+  double load = 0, share = total / grid;
+  d.first.push_back(0);
+  auto next = [&] {
+    d.us = std::max(d.us, load);
+    share += total / grid - load;
+    load = 0;
+    d.first.push_back((int)d.items.size());
+  };
+  double partial = 0;
+  for (const AttnItem& it : items) {
+    int at = it.j0, parts = 0;
+    const int index = (int)d.items.size();
+    for (;;) {
+      AttnItem x = it;
+      x.j0 = at;
+      const bool last = (int)d.first.size() == grid;  // the last CTA takes what is left
+      if (!last && load + item_cost(x) > share + kItemUs / 2) {
+        const int fit = (int)((share - load - kItemUs) / step_cost(it));
+        if (fit < 2 && load > 0) {
+          next();
+          continue;
+        }
+        if (std::max(fit, 2) < x.j1 - x.j0 - 1) x.j1 = x.j0 + std::max(fit, 2);
+      }
+      at = x.j1;
+      if (parts || at < it.j1) x.slot = d.slots++;
+      ++parts;
+      load += item_cost(x);
+      d.items.push_back(x);
+      if (at >= it.j1) break;
+      next();
+    }
+    if (parts > 1) {
+      const int rows = it.alt ? (it.tend - it.t0) * G : 256;
+      d.prows = std::max(d.prows, rows);
+      partial += (double)parts * rows * D * 8;
+      d.merges.push_back(make_int2(index, parts));
+    }
+  }
+  next();
+  if (!d.merges.empty()) d.us += kMergeUs + partial / kMergeBytes;
+  return d;
+}
+
+Division plan_items(const int* q_lens, const int* k_lens, int n, int kvh, int G, int D, bool causal, int num_sms) {
   const int tpt = kAttRows / G;
-  std::vector<AttnItem> whole;
+  std::vector<AttnItem> items;
   long long q0 = 0, k0 = 0;
-  double total = 0;
+  long long tiles = 0;
   for (int s = 0; s < n; ++s) {
     const int ql = q_lens[s], kl = k_lens[s];
     for (int t = 0; t < ql; t += 2 * tpt)
@@ -126,56 +209,24 @@ Division plan_items(const int* q_lens, const int* k_lens, int n, int kvh, int G,
         it.lowB = it.alt ? it.lowA : att_limit(it, it.t0 + tpt);
         it.eA = it.alt ? it.j1 : (att_limit(it, it.t0 + tpt - 1) + kAttTok - 1) / kAttTok;
         it.eB = it.j1;
-        whole.push_back(it);
-        total += item_cost(it);
+        items.push_back(it);
+        tiles += it.j1;
       }
     q0 += ql;
     k0 += kl;
   }
-  // Items longer than an SM's share are cut into parts of about that size (8 units at least:
-  // a part's partial results cost about as much), whose results a second kernel joins.
-  Division d;
-  const double share = std::max(8.0, total / num_sms);
-  std::vector<AttnItem> items;
-  std::vector<int> parts_of;  // of the item that starts a group, else 0
-  for (const AttnItem& it : whole) {
-    const int tiles = it.j1 - it.j0;
-    const int parts = std::max(1, std::min(tiles, (int)std::ceil((item_cost(it) - 3.0) / share)));
-    for (int p = 0; p < parts; ++p) {
-      AttnItem x = it;
-      x.j0 = it.j0 + (int)((long long)tiles * p / parts);
-      x.j1 = it.j0 + (int)((long long)tiles * (p + 1) / parts);
-      if (parts > 1) x.slot = d.slots++;
-      items.push_back(x);
-      parts_of.push_back(parts > 1 && p == 0 ? parts : 0);
-    }
-    if (parts > 1) d.prows = std::max(d.prows, it.alt ? (it.tend - it.t0) * G : 256);
+  Division best = divide_whole(items, num_sms);
+  // Work cut evenly where that is quicker, merge included: on all SMs, or, of little work, on fewer
+  // with more tiles each.
+  for (int least = 2; least <= 8 && !items.empty(); least *= 2) {
+    const int grid = (int)std::min<long long>(num_sms, tiles / least);
+    if (grid < 2) break;
+    Division cut = divide_cut(items, grid, G, D);
+    if (cut.us < best.us) best = std::move(cut);
+    if (grid < num_sms) continue;
+    break;
   }
-  // the longest first, each to the CTA with the least to do (few items: one each)
-  std::vector<int> order(items.size());
-  for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
-  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return item_cost(items[a]) > item_cost(items[b]); });
-  const int grid = (int)std::min<size_t>(items.size(), (size_t)num_sms);
-  std::vector<std::vector<int>> of(grid);
-  using Load = std::pair<double, int>;
-  std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
-  for (int b = 0; b < grid; ++b) least.push({0.0, b});
-  for (int i : order) {
-    Load x = least.top();
-    least.pop();
-    of[x.second].push_back(i);
-    x.first += item_cost(items[i]);
-    least.push(x);
-  }
-  for (int b = 0; b < grid; ++b) {
-    d.first.push_back((int)d.items.size());
-    for (int i : of[b]) {
-      if (parts_of[i]) d.merges.push_back(make_int2((int)d.items.size(), parts_of[i]));
-      d.items.push_back(items[i]);
-    }
-  }
-  d.first.push_back((int)d.items.size());
-  return d;
+  return best;
 }
 
 }  // namespace
@@ -208,7 +259,7 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return prompt_cuda(e, "cudaGetDevice");
-  const dc::Division v = dc::plan_items(q_lens, k_lens, n, kv_heads, q_heads / kv_heads, causal != 0, sms);
+  const dc::Division v = dc::plan_items(q_lens, k_lens, n, kv_heads, q_heads / kv_heads, head_dim, causal != 0, sms);
   // one block on the device: status words, items, each CTA's first item, merges
   auto up = [](size_t x) { return (x + 15) / 16 * 16; };
   const size_t at_items = 64, at_first = up(at_items + v.items.size() * sizeof(dc::AttnItem)),
