@@ -41,7 +41,7 @@ struct AttnArgs {
   float2* part_ml;
   int prows;
   // trees
-  int n, nodes, batch, rows, pairs, tiles, grid;
+  int n, nodes, batch, rows, pairs, tiles, grid, per, extra;
   const int* rowlen;         // each row's length, or null (n)
   const int* parents;        // [batch][nodes]
   unsigned* status;

@@ -84,14 +84,18 @@ __device__ __forceinline__ AttnItem load_item(const AttnArgs& a, int i) {
 // second one, and so on: the CTAs that read a row's keys then do so at the same time) in one
 // line, a.tiles each (the cached tokens', then the drafted ones'; rows may have fewer), of which CTA
 // b of `grid` takes the b-th equal part.
-__host__ __device__ inline long long tree_from(const AttnArgs& a, int b) {
-  return (long long)a.n_items * a.tiles * b / a.grid;
+__host__ __device__ inline int tree_from(const AttnArgs& a, int b) { return b * a.per + (b < a.extra ? b : a.extra); }
+
+// The CTA that takes place `at`.
+__device__ __forceinline__ int tree_cta(const AttnArgs& a, int at) {
+  const int big = a.extra * (a.per + 1);
+  return at < big ? at / (a.per + 1) : a.extra + (at - big) / a.per;
 }
 
 // The item that starts at place `at` of that line, as far as it goes before `end`.
-__device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int b, long long at, long long end) {
-  const int tpt = kAttRows / a.G, i = (int)(at / a.tiles), j0 = (int)(at - (long long)i * a.tiles);
-  const int j1 = (int)(end - at < a.tiles - j0 ? j0 + (end - at) : a.tiles);
+__device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int b, int at, int end) {
+  const int tpt = kAttRows / a.G, i = at / a.tiles, j0 = at - i * a.tiles;
+  const int j1 = min(a.tiles, j0 + end - at);
   AttnItem it;
   it.y = i % a.rows;
   it.lb = it.y / a.kvh;
@@ -293,10 +297,20 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     tmem_alloc(tmem_slot, kAttCols);
     tmem_relinquish();
   }
+  if (warp == 8 && lane == 0) {
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
+    if (TREE) {
+      prefetch_tmap(&tmKD);
+      prefetch_tmap(&tmVD);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  grid_dep_wait();    // all inputs, and the outputs' and partial results' last readers
   grid_dep_launch();  // the partial results' merge, if any, may get ready
   const int tpt = kAttRows / a.G;
 
@@ -314,7 +328,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         const uint64_t pol = TREE && a.pairs == 1 ? l2_evict_first_policy() : l2_evict_normal_policy();
         const uint32_t qbytes = (uint32_t)(tpt * a.G) * (uint32_t)D * 2u;
         int g = 0, sent = 0;
-        long long at = 0, end = 0;
+        int at = 0, end = 0;
         if (TREE) {
           at = tree_from(a, blockIdx.x);
           end = tree_from(a, blockIdx.x + 1);
@@ -330,7 +344,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             next = tree_item(a, blockIdx.x, at, end);
             at = (at / a.tiles + 1) * a.tiles;
           } else {
-            next = load_item(a, (int)at);
+            next = load_item(a, at);
             ++at;
           }
         };
@@ -839,62 +853,107 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   if (threadIdx.x == 0 && *abort) atomicOr(a.status, kStatusTimeout);
 }
 
-// Joins the partial results of the parts of one item, in order: a warp per row. Prompts: `merges`
-// lists each item's first part and their number; trees: merge i belongs to the boundary between
-// CTAs i and i + 1, if that is the first one within its item.
+// Joins the partial results of the parts of one item, in order: block x an item, y 32 of its rows, a
+// warp four of them at once: lane 8 i + s takes m and l of row i's part s (8 parts at a time), then
+// the parts' O come with all loads in flight. Prompts:
+// `merges` lists each item's first part and their number; trees: merge i belongs to the boundary
+// between CTAs i and i + 1, if that is the first one within its item.
 template <class T, int D, bool TREE>
 __global__ void __launch_bounds__(256) merge_kernel(const AttnArgs a) {
+  constexpr int E = D / 32, W = 4;
+  const int lane = threadIdx.x & 31, tpt = kAttRows / a.G, gi = blockIdx.x;
+  AttnItem it;
+  int parts, slot;  // the first part's; the others': the next ones (prompts), or every second from 2 (gi + 1)
+  if constexpr (TREE) {
+    const int cut = tree_from(a, gi + 1), i0 = cut / a.tiles * a.tiles;
+    if (cut == i0 || tree_from(a, gi) > i0) return;
+    it = tree_item(a, gi, i0, i0 + a.tiles);
+    parts = tree_cta(a, i0 + a.tiles - 1) - gi + 1;
+    slot = 2 * gi + 1;
+  } else {
+    const int2 mg = __ldg(a.merges + gi);
+    it = load_item(a, mg.x);
+    parts = mg.y;
+    slot = it.slot;
+  }
+  const int r0 = blockIdx.y * 32 + threadIdx.x / 32 * W;
+  bool valid[W];
+  int tok[W], head[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const int r = r0 + i, rr = r % 128;  // rows of tile A, then of tile B
+    tok[i] = it.t0 + r / 128 * tpt + rr / a.G;
+    head[i] = it.h * a.G + rr % a.G;
+    valid[i] = r < a.prows && rr < tpt * a.G && tok[i] < it.tend;
+  }
   grid_dep_wait();
-  const int lane = threadIdx.x & 31, tpt = kAttRows / a.G;
-  for (long long u = (long long)blockIdx.x * 8 + threadIdx.x / 32; u < (long long)a.n_merges * a.prows;
-       u += (long long)gridDim.x * 8) {
-    const int gi = (int)(u / a.prows), r = (int)(u % a.prows);
-    AttnItem it;
-    int parts;
-    int slot;  // of the first part; the others': every one (prompts), or every second from 2 (b + 1)
-    if constexpr (TREE) {
-      const long long cut = tree_from(a, gi + 1), i0 = cut / a.tiles * a.tiles;
-      if (cut == i0 || tree_from(a, gi) > i0) continue;
-      it = tree_item(a, gi, i0, i0 + a.tiles);
-      parts = 2;
-      while (tree_from(a, gi + parts) < i0 + a.tiles) ++parts;
-      // (a part that starts at its item's start and its CTA's is that CTA's second all the same)
-      slot = 2 * gi + 1;
-    } else {
-      const int2 mg = __ldg(a.merges + gi);
-      it = load_item(a, mg.x);
-      parts = mg.y;
-      slot = it.slot;
-    }
-    auto place = [&](int s) { return (long long)(TREE && s ? 2 * (gi + s) : slot + s) * a.prows; };
-    // rows of tile A, then of tile B
-    const int x = r / 128, rr = r % 128, t = it.t0 + x * tpt + rr / a.G;
-    if (rr >= tpt * a.G || t >= it.tend) continue;
-    const float2* ml = a.part_ml + r;
-    const float* part = a.part + (long long)r * D;
-    float m = -INFINITY, l = 0.f;
-    bool sees = true;
-    for (int s = 0; s < parts; ++s) {
-      const float2 v = ml[place(s)];
-      m = fmaxf(m, v.x);
-      sees = sees && !(v.y < 0.f);
-    }
-    float o[D / 32] = {};
-    for (int s = 0; s < parts && sees; ++s) {
-      const float2 v = ml[place(s)];
-      if (v.x == -INFINITY && v.y == 0.f) continue;
-      const float f = v.x == -INFINITY ? 1.f : ex2((v.x - m) * a.c);
-      l = fmaf(f, v.y, l);
-      const float* p = part + place(s) * D + lane * (D / 32);
+  auto place = [&](int s) { return (long long)(TREE && s ? 2 * (gi + s) : slot + s) * a.prows + r0; };
+  // this lane's row and part
+  const int li = lane / 8, ls = lane % 8;
+  bool lv = false;
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = fmaf(f, p[e], o[e]);
-    }
-    const float inv = sees ? 1.f / l : 0.f;
-    const int head = it.h * a.G + rr % a.G;
-    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + it.lb * a.o_lb + (long long)t * a.o_t + head * a.o_h) + lane * (D / 64);
+  for (int i = 0; i < W; ++i) lv = lv || (i == li && valid[i]);
+  auto load = [&](int s) { return lv && s < parts ? a.part_ml[place(s) + li] : make_float2(-INFINITY, 0.f); };
+  const float2 v0 = load(ls);  // (8 parts or fewer: read once)
+  float mm = v0.x;
+  bool unseen = v0.y < 0.f;
+  for (int s = 8; s < parts; s += 8) {
+    const float2 v = load(s + ls);
+    mm = fmaxf(mm, v.x);
+    unseen = unseen || v.y < 0.f;
+  }
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) to[e] = T::pack(o[2 * e] * inv, o[2 * e + 1] * inv);
-    if (a.lse && lane == 0) a.lse[(long long)t * a.kvh * a.G + head] = sees ? fmaf(m, a.scale, logf(l)) : -INFINITY;
+  for (int x = 1; x < 8; x *= 2) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, x));
+  const uint32_t blind = __ballot_sync(0xffffffffu, unseen);
+  float ll = 0.f, o[W][E] = {};
+  for (int s0 = 0; s0 < parts; s0 += 8) {
+    const float2 v = s0 ? load(s0 + ls) : v0;
+    // (a part of which the row sees nothing has no say, whatever it holds: factor -1)
+    const bool none = v.x == -INFINITY && !(v.y != v.y);
+    const float f = none ? -1.f : v.x == -INFINITY ? 1.f : ex2((v.x - mm) * a.c);
+    if (!none) ll = fmaf(f, v.y, ll);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      if (s0 + s >= parts) break;
+      const float* part = a.part + place(s0 + s) * D + lane * E;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float fi = __shfl_sync(0xffffffffu, f, i * 8 + s);
+        if (!valid[i]) continue;
+        float x[E];
+        if constexpr (E == 4) {
+          const float4 y = *reinterpret_cast<const float4*>(part + (long long)i * D);
+          x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
+        } else {
+          const float2 y = *reinterpret_cast<const float2*>(part + (long long)i * D);
+          x[0] = y.x; x[1] = y.y;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] = fi == -1.f ? o[i][e] : fmaf(fi, x[e], o[i][e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 1; x < 8; x *= 2) ll += __shfl_xor_sync(0xffffffffu, ll, x);
+  float m[W], l[W];
+  bool sees[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    m[i] = __shfl_sync(0xffffffffu, mm, i * 8);
+    l[i] = __shfl_sync(0xffffffffu, ll, i * 8);
+    sees[i] = (blind >> (i * 8) & 0xffu) == 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    if (!valid[i]) continue;
+    const float inv = sees[i] ? rcp(l[i]) : 0.f;
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + it.lb * a.o_lb + (long long)tok[i] * a.o_t + head[i] * a.o_h) + lane * (E / 2);
+    uint32_t w[E / 2];
+#pragma unroll
+    for (int e = 0; e < E; e += 2) w[e / 2] = sees[i] ? T::pack(o[i][e] * inv, o[i][e + 1] * inv) : 0u;
+    if constexpr (E == 4) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+    else *to = w[0];
+    if (a.lse && lane == 0) a.lse[(long long)tok[i] * a.kvh * a.G + head[i]] = sees[i] ? fmaf(m[i], a.scale, logf(l[i])) : -INFINITY;
   }
 }
 
@@ -904,15 +963,16 @@ struct AttMaps {
 };
 
 template <class T, int D, bool TREE>
-cudaError_t launch_attend(const AttMaps& m, const AttnArgs& a, int grid, int num_sms, cudaStream_t s) {
+cudaError_t launch_attend(const AttMaps& m, const AttnArgs& a, int grid, cudaStream_t s) {
   static SmemLimit limit;
   if (cudaError_t e = limit.raise(attend_kernel<T, D, TREE>, AttSmem<D>::BYTES); e != cudaSuccess) return e;
-  attend_kernel<T, D, TREE><<<grid, kAttThreads, AttSmem<D>::BYTES, s>>>(m.q, m.k, m.v, m.kd, m.vd, a);
-  if (cudaError_t e = cudaGetLastError(); e != cudaSuccess) return e;
+  // (its set-up may run under the end of the kernel before it)
+  if (cudaError_t e = launch_pdl(attend_kernel<T, D, TREE>, dim3(grid), dim3(kAttThreads), AttSmem<D>::BYTES, s, m.q, m.k, m.v,
+                                 m.kd, m.vd, a);
+      e != cudaSuccess)
+    return e;
   if (a.n_merges == 0) return cudaSuccess;
-  const long long blocks = ((long long)a.n_merges * a.prows + 7) / 8;
-  return launch_pdl(merge_kernel<T, D, TREE>, dim3((unsigned)(blocks < 8ll * num_sms ? blocks : 8ll * num_sms)), dim3(256),
-                    0, s, a);
+  return launch_pdl(merge_kernel<T, D, TREE>, dim3((unsigned)a.n_merges, (unsigned)((a.prows + 31) / 32)), dim3(256), 0, s, a);
 }
 
 }  // namespace

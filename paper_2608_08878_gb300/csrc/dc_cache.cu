@@ -1049,6 +1049,7 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   a.status = p.status;
   a.dbg = p.dbg;
   const long long slots = dc::tree_plan(&a, h->num_sms);
+  if (slots < 0) return fail(h, DC_ERR_INVALID_ARG, "too many tokens");
   if (slots) {
     // the partial results of rows in parts: kept with the handle, and made larger when a call needs more
     const size_t rows = (size_t)slots * a.prows;
@@ -1067,7 +1068,7 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   const char* why = nullptr;
   {
     Phase ph(h, DC_PHASE_FULL, slots ? 2 : 1);
-    e = dc::launch_tree(a, p.d, p.stride, h->num_sms, h->stream, &why);
+    e = dc::launch_tree(a, p.d, p.stride, h->stream, &why);
   }
   if (why) return fail(h, DC_ERR_INVALID_ARG, why);
   if (e != cudaSuccess) return cuda_fail(h, e, "tree attention");

@@ -373,11 +373,11 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   m.kd = m.k;
   m.vd = m.v;
   if (D == 128)
-    e = bf ? dc::launch_attend<dc::TypeBf16, 128, false>(m, a, p->grid, p->num_sms, s)
-           : dc::launch_attend<dc::TypeHalf, 128, false>(m, a, p->grid, p->num_sms, s);
+    e = bf ? dc::launch_attend<dc::TypeBf16, 128, false>(m, a, p->grid, s)
+           : dc::launch_attend<dc::TypeHalf, 128, false>(m, a, p->grid, s);
   else
-    e = bf ? dc::launch_attend<dc::TypeBf16, 64, false>(m, a, p->grid, p->num_sms, s)
-           : dc::launch_attend<dc::TypeHalf, 64, false>(m, a, p->grid, p->num_sms, s);
+    e = bf ? dc::launch_attend<dc::TypeBf16, 64, false>(m, a, p->grid, s)
+           : dc::launch_attend<dc::TypeHalf, 64, false>(m, a, p->grid, s);
   if (e != cudaSuccess) return prompt_cuda(e, "launch");
   return DC_OK;
 }

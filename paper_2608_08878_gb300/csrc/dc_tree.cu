@@ -12,19 +12,22 @@ long long tree_plan(AttnArgs* a, int num_sms) {
   a->prows = a->nodes <= tpt ? a->nodes * a->G : 256;
   a->n_items = a->rows * a->pairs;
   a->tiles = (a->n + kAttTok - 1) / kAttTok + 1;
-  const long long total = (long long)a->n_items * a->tiles;
+  const long long total = (long long)a->n_items * a->tiles;  // (8 million at most in this GPU's memory)
+  if (total >= 1ll << 30) return -1;
   // CTAs: every SM an equal share of all key tiles, but at least 2 tiles; or, of few items,
   // one each, where the items are so short that parts would not pay for the merge (about 6 tiles).
   int grid = (int)std::min<long long>(num_sms, std::max<long long>(1, total / 2));
   if (a->n_items <= num_sms && (a->tiles <= 8 || a->n_items == num_sms)) grid = a->n_items;
   a->grid = grid;
+  a->per = (int)(total / grid);
+  a->extra = (int)(total % grid);
   bool cut = false;
   for (int b = 1; b < grid && !cut; ++b) cut = tree_from(*a, b) % a->tiles != 0;
   a->n_merges = cut ? grid - 1 : 0;
   return cut ? 2ll * grid : 0;
 }
 
-cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, int num_sms, cudaStream_t s, const char** why) {
+cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, cudaStream_t s, const char** why) {
   AttMaps m;
   const bool ok = att_map_q(&m.q, true, a, D, a.nodes, a.rows / a.kvh) &&
                   att_map_kv(&m.k, true, a.k, D, a.rows, a.k_y, tokens, a.k_t) &&
@@ -35,8 +38,8 @@ cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, int num_sms,
     *why = "cuTensorMapEncodeTiled rejected the layout";
     return cudaErrorInvalidValue;
   }
-  return D == 128 ? launch_attend<TypeBf16, 128, true>(m, a, a.grid, num_sms, s)
-                  : launch_attend<TypeBf16, 64, true>(m, a, a.grid, num_sms, s);
+  return D == 128 ? launch_attend<TypeBf16, 128, true>(m, a, a.grid, s)
+                  : launch_attend<TypeBf16, 64, true>(m, a, a.grid, s);
 }
 
 }  // namespace dc
