@@ -359,25 +359,38 @@ def _fresh(t, name: str, shape) -> None:
         raise DCError(DC_ERR_INVALID_ARG, f"{name}'s elements overlap (strides {tuple(t.stride())})")
 
 
-def _run_on(device: int, stream, tensors, call):
-    """call(stream handle) with `device` current, on `stream` or the device's current stream. With a stream given it
-    is made current, so that what the call allocates belongs to it, and tensors made on another are told that
-    this one uses them."""
+def _raw_stream(device: int) -> int:
+    """The handle of the device's current stream (torch.cuda.current_stream() makes an object of it, 1 us)."""
     import torch
-    if stream is None:
-        if torch.cuda.current_device() == device:
-            return call(torch.cuda.current_stream(device).cuda_stream)
-        with torch.cuda.device(device):
-            return call(torch.cuda.current_stream(device).cuda_stream)
-    if stream.device.index != device:
-        raise DCError(DC_ERR_INVALID_ARG, f"stream is on {stream.device}, the tensors on cuda:{device}")
-    with torch.cuda.device(device):
-        if stream != torch.cuda.current_stream(device):
-            for t in tensors:
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+class _elsewhere:
+    """Makes a device current, and a stream if one is given, so that what a call allocates belongs to it; tensors
+    made on another stream are told that this one uses them. Gives the stream's handle."""
+
+    def __init__(self, device: int, stream, tensors):
+        import torch
+        if stream is not None and stream.device.index != device:
+            raise DCError(DC_ERR_INVALID_ARG, f"stream is on {stream.device}, the tensors on cuda:{device}")
+        self.device, self.stream, self.tensors = torch.cuda.device(device), stream, tensors
+        self.index, self.on = device, torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self.device.__enter__()
+        if self.stream is None:
+            return _raw_stream(self.index)
+        if self.stream.cuda_stream != _raw_stream(self.index):
+            for t in self.tensors:
                 if t is not None:
-                    t.record_stream(stream)
-        with torch.cuda.stream(stream):
-            return call(stream.cuda_stream)
+                    t.record_stream(self.stream)
+        self.on.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *a):
+        if self.stream is not None:
+            self.on.__exit__(*a)
+        self.device.__exit__(*a)
 
 
 def _dtype16(t, name: str) -> int:
@@ -423,19 +436,28 @@ def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps:
         to_k = _heads(k_out, "k_out", hk, d, dtype, dev)
         _fresh(k_out, "k_out", k.shape)
 
-    def call(s):
-        qo = torch.empty((T, hq, d), dtype=dtype, device=q.device) if q_out is None else q_out
-        ko = torch.empty((T, hk, d), dtype=dtype, device=q.device) if k_out is None else k_out
-        tq = (qo.data_ptr(), hq * d, d) if q_out is None else to_q
-        tk = (ko.data_ptr(), hk * d, d) if k_out is None else to_k
-        a = dc_rotate_args(T, hq, hk, d, 2 * pairs, kind, 1 if norm else 0, 1 if interleaved else 0, eps, pos, freq, wq, wk,
-                           at_q[0], at_k[0], tq[0], tk[0], at_q[1], at_q[2], at_k[1], at_k[2], tq[1], tq[2], tk[1], tk[2])
-        st = lib().dc_norm_rotate(a, s)
-        if st != DC_OK:
-            raise DCError(st, lib().dc_rotate_last_error().decode())
-        return qo, ko
-
-    return _run_on(dev, stream, (q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out), call)
+    if stream is None and torch.cuda.current_device() == dev:
+        s, here = _raw_stream(dev), None
+    else:
+        here = _elsewhere(dev, stream, (q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out))
+        s = here.__enter__()
+    try:
+        if q_out is None:
+            q_out = torch.empty((T, hq, d), dtype=dtype, device=q.device)
+            to_q = q_out.data_ptr(), hq * d, d
+        if k_out is None:
+            k_out = torch.empty((T, hk, d), dtype=dtype, device=q.device)
+            to_k = k_out.data_ptr(), hk * d, d
+        L = lib()
+        st = L.dc_norm_rotate(dc_rotate_args(T, hq, hk, d, 2 * pairs, kind, 1 if norm else 0, 1 if interleaved else 0, eps,
+                                             pos, freq, wq, wk, at_q[0], at_k[0], to_q[0], to_k[0], at_q[1], at_q[2],
+                                             at_k[1], at_k[2], to_q[1], to_q[2], to_k[1], to_k[2]), s)
+    finally:
+        if here is not None:
+            here.__exit__(None, None, None)
+    if st != DC_OK:
+        raise DCError(st, L.dc_rotate_last_error().decode())
+    return q_out, k_out
 
 
 class PromptPlan:
@@ -496,17 +518,25 @@ class PromptPlan:
             _fresh(out, "out", q.shape)
             _arg(out, "out", dtype, q.numel(), device=dev)
 
-        def call(s):
-            o = torch.empty(q.shape, dtype=dtype, device=q.device) if out is None else out
+        if stream is None and torch.cuda.current_device() == dev:
+            s, here = _raw_stream(dev), None
+        else:
+            here = _elsewhere(dev, stream, (q, k, v, out))
+            s = here.__enter__()
+        try:
+            if out is None:
+                out = torch.empty(q.shape, dtype=dtype, device=q.device)
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
             need = self.workspace_bytes
             work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-            a = dc_prompt_args(kind, 1.0 / d ** 0.5 if scale is None else scale, at_q[0], at_k[0], at_v[0], at_q[1], at_q[2],
-                               at_k[1], at_k[2], at_v[1], at_v[2], o.data_ptr(), _ptr(lse), _ptr(work), need)
-            self._ok(lib().dc_prompt_attend(self._p, a, s))
-            return (o, lse) if with_lse else o
-
-        return _run_on(dev, stream, (q, k, v, out), call)
+            st = lib().dc_prompt_attend(self._p, dc_prompt_args(
+                kind, 1.0 / d ** 0.5 if scale is None else scale, at_q[0], at_k[0], at_v[0], at_q[1], at_q[2], at_k[1],
+                at_k[2], at_v[1], at_v[2], out.data_ptr(), _ptr(lse), _ptr(work), need), s)
+        finally:
+            if here is not None:
+                here.__exit__(None, None, None)
+        self._ok(st)
+        return (out, lse) if with_lse else out
 
     def check(self, stream=None) -> None:
         """Waits for the stream; raises if a kernel of this plan reported an error."""
@@ -676,7 +706,7 @@ class DistillCache:
         pk = _arg(k_draft, "k_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         pv = _arg(v_draft, "v_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         if out is None:
-            if torch.cuda.current_stream(self.device) == self.stream:
+            if _raw_stream(self.device) == self.stream.cuda_stream:
                 out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
             else:  # (what the cache's stream writes belongs to that stream)
                 with torch.cuda.stream(self.stream):
