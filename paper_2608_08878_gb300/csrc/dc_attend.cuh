@@ -40,6 +40,7 @@ struct AttnArgs {
   float* part;
   float2* part_ml;
   int prows;
+  long long out_len, part_rows;  // debug builds: elements of out, rows of part
   // trees
   int n, nodes, batch, rows, pairs, tiles, grid, per, extra;
   const int* rowlen;         // each row's length, or null (n)
@@ -135,15 +136,17 @@ __device__ __noinline__ void attend_row(const AttnArgs& a, const uint16_t* q, co
   l = 0.f;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-  for (int pass = 0; pass < 2; ++pass) {
+  // the largest score, then the sums
+  auto best = [&](const uint16_t* kj) { m = fmaxf(m, dot(kj)); };
+#pragma unroll 4
+  for (int j = j0; j < j1; ++j) best(k + j * a.k_t);
+  if (w)
+    for (int j = 0; j < a.nodes; ++j)
+      if (w[j >> 5] >> (j & 31) & 1u) best(kd + (long long)j * D);
+  {
     const float mc = m == -INFINITY ? 0.f : m * a.c;
     auto key = [&](const uint16_t* kj, const uint16_t* vj) {
-      const float s = dot(kj);
-      if (pass == 0) {
-        m = fmaxf(m, s);
-        return;
-      }
-      const float p = exp2f(fmaf(s, a.c, -mc));
+      const float p = exp2f(fmaf(dot(kj), a.c, -mc));
       l += p;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -152,6 +155,7 @@ __device__ __noinline__ void attend_row(const AttnArgs& a, const uint16_t* q, co
         o[2 * e + 1] = fmaf(p, f.y, o[2 * e + 1]);
       }
     };
+#pragma unroll 4
     for (int j = j0; j < j1; ++j) key(k + j * a.k_t, v + j * a.v_t);
     if (w)
       for (int j = 0; j < a.nodes; ++j)

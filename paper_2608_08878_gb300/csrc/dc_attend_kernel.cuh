@@ -58,6 +58,8 @@ constexpr int kAttThreads = 384;
 constexpr int kAttRegsRow = 216, kAttRegsIssue = 72;
 constexpr int kAttCols = 512;
 constexpr int kItemRing = 4;  // items published ahead
+// Longer than mbar_wait's own limit: the other roles wait while attend_row goes over a long row.
+constexpr uint64_t kAttWaitNs = 10000000000ull;
 
 template <int D>
 struct AttSmem {
@@ -140,6 +142,11 @@ struct Steps {
   // steps of A (x = 0) or B
   __device__ __forceinline__ int count(int x) const { return alt ? (n + 1 - x) / 2 : max(0, n - (x ? skipB : skipA)); }
 };
+
+__device__ __forceinline__ bool att_wait(uint64_t* bar, uint32_t parity, volatile int* abort, unsigned* dbg, unsigned site,
+                                         unsigned info) {
+  return mbar_wait(bar, parity, abort, dbg, site, info, kAttWaitNs);
+}
 
 // What the producer tells the other warps of an item.
 struct Published {
@@ -317,7 +324,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   // Waits for published item number k; false: no more, or the wait gave up.
   auto ready = [&](int k, unsigned site) {
     const int e = k % kItemRing;
-    return mbar_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k) && ring[e].it.y >= 0;
+    return att_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k) && ring[e].it.y >= 0;
   };
 
   if (warp >= 8) {
@@ -352,7 +359,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         for (int k = 0; !*abort; ++k) {
           const AttnItem it = next;
           const int e = k % kItemRing;
-          if (!mbar_wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, abort, a.dbg, 200u, (unsigned)k)) break;
+          if (!att_wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, abort, a.dbg, 200u, (unsigned)k)) break;
           int4* p = reinterpret_cast<int4*>(ring + e);
           p[0] = make_int4(it.y, it.h, it.lb, it.t0);
           p[1] = make_int4(it.tend, it.k0, it.klen, it.off);
@@ -365,7 +372,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           if (it.y < 0) break;
           fetch();
           if (st.n == 0) continue;
-          if (!mbar_wait(b_qempty, (sent & 1) ^ 1, abort, a.dbg, 201u, (unsigned)k)) break;
+          if (!att_wait(b_qempty, (sent & 1) ^ 1, abort, a.dbg, 201u, (unsigned)k)) break;
           mbar_expect_tx(b_qfull, st.alt ? qbytes : 2 * qbytes);
           for (int x = 0; x < (st.alt ? 1 : 2); ++x)
             for (int c = 0; c < D / 64; ++c)
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           ++sent;
           auto load = [&](int j, bool v) {
             const int s = g % ST;
-            if (!mbar_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, a.dbg, 202u, (unsigned)g)) return;
+            if (!att_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, a.dbg, 202u, (unsigned)g)) return;
             mbar_expect_tx(&b_full[s], L::TILE);
             const bool d = TREE && j == st.draft;
             const CUtensorMap* tm = d ? (v ? &tmVD : &tmKD) : v ? &tmV : &tmK;
@@ -409,10 +416,10 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             mbar_arrive(&b_free[k % kItemRing]);
             continue;
           }
-          ok = mbar_wait(b_qfull, items, abort, a.dbg, 204u, (unsigned)k);
+          ok = att_wait(b_qfull, items, abort, a.dbg, 204u, (unsigned)k);
           if (!ok) break;
           items ^= 1u;
-          auto full = [&](const Place<ST>& p) { return mbar_wait(&b_full[p.s], p.phase, abort, a.dbg, 205u, (unsigned)k); };
+          auto full = [&](const Place<ST>& p) { return att_wait(&b_full[p.s], p.phase, abort, a.dbg, 205u, (unsigned)k); };
           auto s_mma = [&](int x, uint32_t qlo, uint32_t stage) {
             const uint32_t klo = k_lo + stage * (L::TILE >> 4);
 #pragma unroll
@@ -426,7 +433,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             const uint32_t vlo = v_lo + stage * (L::TILE >> 4);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              if (!mbar_wait(&b_p[2 * x + h], np[x], abort, a.dbg, 206u, (unsigned)k)) return false;
+              if (!att_wait(&b_p[2 * x + h], np[x], abort, a.dbg, 206u, (unsigned)k)) return false;
               tc_fence_after();
 #pragma unroll
               for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
@@ -522,7 +529,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         int found = 0;
         bool ok = true;
         auto pass = [&](int i) {  // i >= 0: V of step i, else some K
-          ok = __all_sync(0xffffffffu, ok && mbar_wait(&b_full[g.s], g.phase, abort, a.dbg, 208u, (unsigned)k));
+          ok = __all_sync(0xffffffffu, ok && att_wait(&b_full[g.s], g.phase, abort, a.dbg, 208u, (unsigned)k));
           const int mk = ok && i >= 0 ? st.masked(i) : 0;
           if (mk) {
             // the keys that some row must not see
@@ -592,7 +599,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       const int jstep = TREE ? alt + 1 : -1 - alt;
 #pragma unroll 1
       for (int i = 0; i < steps; ++i, j += jstep) {
-        mbar_wait(&b_s[X], ns, abort, a.dbg, 210u + X, (unsigned)k);
+        att_wait(&b_s[X], ns, abort, a.dbg, 210u + X, (unsigned)k);
         ns ^= 1u;
         if (busy) {
           tc_fence_after();
@@ -692,7 +699,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
 
       // ---------------------------------------------------------- the item's result
       // (all that does not need O goes before the wait for it)
-      mbar_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, a.dbg, 214u, (unsigned)k);
+      att_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, a.dbg, 214u, (unsigned)k);
       const int found = flags[2 * (k % kItemRing)] | flags[2 * (k % kItemRing) + 1];
       const bool bad = alt ? found != 0 : (found >> X & 1) != 0;
       // of two results over the same rows, each warpgroup joins half the dims
@@ -702,7 +709,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         xch[X * 128 + row] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(&b_x[0]);
-        mbar_wait(&b_x[0], nx, abort, a.dbg, 215u, (unsigned)k);
+        att_wait(&b_x[0], nx, abort, a.dbg, 215u, (unsigned)k);
         const float2 y = xch[(X ^ 1) * 128 + row];
         const float mm = fmaxf(m, y.x);
         other = ring[k % kItemRing].of[X ^ 1].z;
@@ -724,28 +731,34 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         }
         return x;
       };
+      // (debug builds: whether the row's place lies within the output or the partial results)
+      auto fits = [&](int tok, int hd, int r) {
+        return slot >= 0 ? DC_INB(a, (long long)slot * a.prows + r, a.part_rows, 320)
+                         : DC_INB(a, it.lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h + D - 1, a.out_len, 321);
+      };
       const int head = it.h * a.G + row_g, prow = (alt ? 0 : X * 128) + row;
       RowOut ro = place(t, head, prow);
       ro.sees = sees;
+      const bool writes = valid && fits(t, head, prow);
       // where this lane's share of the rows goes
       uint8_t* to[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         to[i] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(ro.out),
                                                        i * 4 + lane / 8)) + (lane & 7) * 16;
-      const uint32_t on = __ballot_sync(0xffffffffu, valid);
-      if (!bad && valid && (!alt || X == 0)) ro.stats(a, m, l);
+      const uint32_t on = __ballot_sync(0xffffffffu, writes);
+      if (!bad && writes && (!alt || X == 0)) ro.stats(a, m, l);
       {
         const float inv = slot >= 0 ? 1.f : sees ? rcp(l) : 0.f;
         f *= inv;
         fy *= inv;
       }
       if (steps) {
-        mbar_wait(&b_o[X], no, abort, a.dbg, 212u + X, (unsigned)k);
+        att_wait(&b_o[X], no, abort, a.dbg, 212u + X, (unsigned)k);
         no ^= 1u;
       }
       // (the other's products: it has passed its earlier results, as its part of the exchange says)
-      if (other) mbar_wait(&b_o[X ^ 1], oo, abort, a.dbg, 213u, (unsigned)k);
+      if (other) att_wait(&b_o[X ^ 1], oo, abort, a.dbg, 213u, (unsigned)k);
       oo ^= ring[k % kItemRing].of[X ^ 1].z ? 1u : 0u;
       tc_fence_after();
       if (bad) {
@@ -753,7 +766,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         // (of two results over the same rows, by the first warpgroup)
         if (!(alt && X == 1)) {
           for (int rr = 0; rr < 32; ++rr) {
-            if (!__shfl_sync(0xffffffffu, (int)valid, rr)) continue;
+            if (!__shfl_sync(0xffffffffu, (int)writes, rr)) continue;
             const int tok = __shfl_sync(0xffffffffu, t, rr), hd = __shfl_sync(0xffffffffu, head, rr);
             const int see = __shfl_sync(0xffffffffu, lim, rr);
             uint32_t w[4];
@@ -839,7 +852,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       if (alt) {
         // the other warpgroup has read this one's O and statistics before they are written again
         if (lane == 0) mbar_arrive(&b_x[1]);
-        mbar_wait(&b_x[1], nx, abort, a.dbg, 216u, (unsigned)k);
+        att_wait(&b_x[1], nx, abort, a.dbg, 216u, (unsigned)k);
         nx ^= 1u;
       }
       if (lane == 0) mbar_arrive(&b_free[k % kItemRing]);
@@ -884,7 +897,9 @@ __global__ void __launch_bounds__(256) merge_kernel(const AttnArgs a) {
     const int r = r0 + i, rr = r % 128;  // rows of tile A, then of tile B
     tok[i] = it.t0 + r / 128 * tpt + rr / a.G;
     head[i] = it.h * a.G + rr % a.G;
-    valid[i] = r < a.prows && rr < tpt * a.G && tok[i] < it.tend;
+    valid[i] = r < a.prows && rr < tpt * a.G && tok[i] < it.tend &&
+               DC_INB(a, it.lb * a.o_lb + (long long)tok[i] * a.o_t + head[i] * a.o_h + D - 1, a.out_len, 322) &&
+               DC_INB(a, (long long)slot * a.prows + r, a.part_rows, 323);
   }
   grid_dep_wait();
   auto place = [&](int s) { return (long long)(TREE && s ? 2 * (gi + s) : slot + s) * a.prows + r0; };

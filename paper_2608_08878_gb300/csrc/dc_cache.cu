@@ -98,9 +98,8 @@ struct dc_cache {
   dc::Step gstep{};
   unsigned gepoch = 0;
   int* gcount_dev = nullptr;
-  // partial results of dc_tree_attend's rows in parts (floats)
+  // partial results of dc_tree_attend's rows in parts
   float* tree_part = nullptr;
-  size_t tree_len = 0;
   struct Alloc {
     void* base;    // what cudaMalloc returned (guard regions included in debug builds)
     size_t bytes;  // the buffer's own size
@@ -1051,19 +1050,27 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   const long long slots = dc::tree_plan(&a, h->num_sms);
   if (slots < 0) return fail(h, DC_ERR_INVALID_ARG, "too many tokens");
   if (slots) {
-    // the partial results of rows in parts: kept with the handle, and made larger when a call needs more
-    const size_t rows = (size_t)slots * a.prows;
-    if (rows * (p.d + 2) > h->tree_len) {
-      float* buf = nullptr;
-      cudaError_t ae = dalloc(h, &buf, rows * (p.d + 2) * sizeof(float));
-      if (ae != cudaSuccess) return alloc_fail(h, ae, "tree attention");
-      dfree(h, &h->tree_part);
-      h->tree_part = buf;
-      h->tree_len = rows * (p.d + 2);
+    // the partial results of rows in parts: one buffer for any call (two parts a CTA at most), made by
+    // the first call that needs it, since a captured graph may hold its address
+    const size_t rows = (size_t)2 * h->num_sms * 2 * dc::kAttRows;
+    if (!h->tree_part) {
+      cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+      if (cudaStreamIsCapturing(h->stream, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone) {
+        cudaGetLastError();
+        return fail(h, DC_ERR_STATE, "the first call allocates: make one before a stream capture");
+      }
+      cudaError_t ae = dalloc(h, &h->tree_part, rows * (p.d + 2) * sizeof(float));
+      if (ae != cudaSuccess) {
+        cudaStreamSynchronize(h->stream);
+        dfree(h, &h->tree_part);
+        return alloc_fail(h, ae, "tree attention");
+      }
     }
     a.part = h->tree_part;
     a.part_ml = reinterpret_cast<float2*>(h->tree_part + rows * p.d);
+    a.part_rows = slots * a.prows;
   }
+  a.out_len = (long long)(p.R / p.kvh) * a.o_lb;
   cudaError_t e;
   const char* why = nullptr;
   {

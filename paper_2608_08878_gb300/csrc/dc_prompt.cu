@@ -357,6 +357,8 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   a.n_merges = p->n_merges;
   a.prows = p->prows;
   a.part = (float*)x.workspace;
+  a.part_rows = (long long)p->n_slots * p->prows;
+  a.out_len = p->q_tokens * a.o_t;
   a.part_ml = (float2*)((float*)x.workspace + (size_t)p->n_slots * p->prows * p->head_dim);
   a.status = p->status;
   a.dbg = p->status + 8;

@@ -55,6 +55,7 @@ def run(q_lens, kvh, group, d, dtype=BF, k_lens=None, causal=True, seed=0):
     q, k, v = inputs(q_lens, k_lens, kvh, group, d, dtype, seed)
     plan = dc.PromptPlan(q_lens, kvh, d, q_heads=kvh * group, k_lens=k_lens, causal=causal)
     out, lse = plan.attend(q, k, v, with_lse=True)
+    plan.check()
     assert out.dtype == dtype and lse.dtype == torch.float32
     compare(out, lse, q, k, v, q_lens, k_lens, causal)
 
@@ -217,6 +218,47 @@ def test_same_results_every_time_on_every_stream_and_from_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_refusals():
+    q, k, v = inputs([8], [8], 2, 2, 64, BF)
+    plan = dc.PromptPlan([8], 2, 64, q_heads=4)
+    odd = torch.zeros(8 * 4 * 64 + 1, dtype=BF, device="cuda")[1:].view(8, 4, 64)
+    bad = {
+        "q of another type": lambda: plan.attend(q.float(), k, v),
+        "k of another type": lambda: plan.attend(q, k.half(), v),
+        "k on the host": lambda: plan.attend(q, k.cpu(), v),
+        "one token short": lambda: plan.attend(q[:7], k, v),
+        "v one token short": lambda: plan.attend(q, k, v[:7]),
+        "another head count": lambda: plan.attend(q[:, :2], k, v),
+        "another head size": lambda: plan.attend(q[..., :32], k[..., :32], v[..., :32]),
+        "heads off 16 bytes": lambda: plan.attend(odd, k, v),
+        "one key for all tokens": lambda: plan.attend(q, k[:1].expand(8, 2, 64), v),
+        "an output of another shape": lambda: plan.attend(q, k, v, out=q[:7]),
+        "an output that is not dense": lambda: plan.attend(q, k, v, out=q.transpose(0, 1)),
+        "scale 0": lambda: plan.attend(q, k, v, scale=0.0),
+        "a scale that is not finite": lambda: plan.attend(q, k, v, scale=math.inf),
+    }
+    for what, call in bad.items():
+        with pytest.raises(dc.DCError) as e:
+            call()
+        assert e.value.status == dc.DC_ERR_INVALID_ARG, what
+    compare(plan.attend(q, k, v), None, q, k, v, [8], [8])
+    plan.close()
+    with pytest.raises(dc.DCError):
+        plan.attend(q, k, v)
+
+
+def test_the_workspace_is_checked():
+    """A plan that divides long key sequences needs its workspace: none, too small and off 16 bytes are refused."""
+    import ctypes as C
+    q, k, v = inputs([1], [20000], 1, 4, 64, BF)
+    plan = dc.PromptPlan([1], 1, 64, q_heads=4, k_lens=[20000])
+    assert plan.workspace_bytes > 0
+    out, work = torch.empty_like(q), torch.empty(plan.workspace_bytes + 16, dtype=torch.uint8, device="cuda")
+    for at, n in ((0, plan.workspace_bytes), (work.data_ptr(), plan.workspace_bytes - 1), (work.data_ptr() + 8, plan.workspace_bytes)):
+        a = dc.dc_prompt_args(0, 0.125, q.data_ptr(), k.data_ptr(), v.data_ptr(), 256, 64, 64, 64, 64, 64, out.data_ptr(), 0, at, n)
+        assert dc.lib().dc_prompt_attend(plan._p, C.byref(a), None) == dc.DC_ERR_INVALID_ARG
 
 
 def test_random_shapes():

@@ -180,6 +180,43 @@ def test_refusals():
     compare(cache, (q, kd, vd, parents), cache.tree_attend(q, kd, vd, parents))
 
 
+def test_a_captured_call_replays():
+    """A row in parts: the first call makes the buffer for them, so it is refused in a capture; a later one is captured
+    and replays on what its tensors then hold."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        cache, (q, kd, vd, parents) = make(1, 1, 2, 4, 64, 5000, 4)
+        out = torch.zeros_like(q)
+        cache.sync()
+        refused = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(refused, stream=stream):
+            out.add_(0)
+            with pytest.raises(dc.DCError) as e:
+                cache.tree_attend(q, kd, vd, parents, out)
+        assert e.value.status == dc.DC_ERR_STATE
+        cache.tree_attend(q, kd, vd, parents, out)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            cache.tree_attend(q, kd, vd, parents, out)
+        q.copy_(rand(1, 1, 4, 8, 64, seed=77))
+        graph.replay()
+        stream.synchronize()
+        compare(cache, (q, kd, vd, parents), out)
+
+
+def test_an_allocation_failure_leaves_the_cache_usable():
+    cache, draft = make(1, 1, 2, 4, 64, 5000, 4)
+    try:
+        dc.debug_fail_alloc(0)
+        with pytest.raises(dc.DCError) as e:
+            cache.tree_attend(*draft)
+        assert e.value.status == dc.DC_ERR_OOM
+    finally:
+        dc.debug_fail_alloc(-1)
+    compare(cache, draft, cache.tree_attend(*draft))
+    cache.sync()
+
+
 def test_graph_mode_refuses():
     cache, draft = make(1, 1, 2, 4, 64, 130, 3, window=2)
     for i in range(3):
