@@ -337,6 +337,8 @@ extern "C" dc_status dc_norm_rotate(const dc_rotate_args* args, void* stream) {
                        (a.kv_heads ? a.k_token_stride | a.k_head_stride | a.k_out_token_stride | a.k_out_head_stride : 0);
   if ((at & 15) || (st & 7))
     return rotate_fail(DC_ERR_INVALID_ARG, "q, k and their outputs must start every head on 16 bytes (strides multiples of 8)");
+  if (((uintptr_t)a.positions | (uintptr_t)a.inv_freq | (uintptr_t)a.q_weight | (uintptr_t)a.k_weight) & 3)
+    return rotate_fail(DC_ERR_INVALID_ARG, "positions, inv_freq and weights must be 4-byte aligned");
   const int sms = dc::sm_count();
   if (sms < 1) return rotate_fail(DC_ERR_CUDA, "no CUDA device");
   const cudaStream_t s = static_cast<cudaStream_t>(stream);

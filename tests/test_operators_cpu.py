@@ -29,7 +29,7 @@ def _rotate(**kw):
     ("tokens", -1), ("tokens", 1 << 40), ("q_heads", -1), ("kv_heads", 70000), ("head_dim", 60), ("head_dim", 264),
     ("head_dim", 8), ("rotary_dim", 0), ("rotary_dim", 24), ("rotary_dim", 80), ("dtype", 2), ("eps", -1.0),
     ("eps", float("nan")), ("positions", None), ("inv_freq", None), ("q", None), ("k_out", None), ("q", 72), ("k_out", 8),
-    ("q_token_stride", 130), ("k_out_head_stride", 4)])
+    ("q_token_stride", 130), ("k_out_head_stride", 4), ("positions", 66), ("inv_freq", 65), ("q_weight", 2), ("k_weight", 67)])
 def test_norm_rotate_refuses(field, value):
     assert _rotate(**{field: value}) == dc.DC_ERR_INVALID_ARG
     assert dc.lib().dc_rotate_last_error()
