@@ -139,13 +139,38 @@ struct Steps {
     const int w = alt ? 1 << (i & 1) : (i >= skipA ? 1 : 0) | (i >= skipB ? 2 : 0);
     return (w & 1 && masked(i, 0) ? 1 : 0) | (w & 2 && masked(i, 1) ? 2 : 0);
   }
+  // load p of the item's 2 n: V or K of which step. K0 V0 K1 V1 ..., or, where A and B take steps in
+  // turn, K0 K1 V0 K2 V1 K3 ...: as the products take them
+  __device__ __forceinline__ int load(int p, bool& v) const {
+    if (!alt) {
+      v = p & 1;
+      return p >> 1;
+    }
+    const bool last = p == 2 * n - 1;
+    v = last || (p >= 2 && !(p & 1));
+    return last ? n - 1 : v ? (p - 2) >> 1 : p < 2 ? p : (p + 1) >> 1;
+  }
   // steps of A (x = 0) or B
   __device__ __forceinline__ int count(int x) const { return alt ? (n + 1 - x) / 2 : max(0, n - (x ? skipB : skipA)); }
 };
 
-__device__ __forceinline__ bool att_wait(uint64_t* bar, uint32_t parity, volatile int* abort, unsigned* dbg, unsigned site,
-                                         unsigned info) {
-  return mbar_wait(bar, parity, abort, dbg, site, info, kAttWaitNs);
+// Waits as mbar_wait does, in few instructions: what gave up is kept in *abort and recorded at the
+// end. Items of few steps run through most of the kernel's code (100 KB of it), so that its size
+// counts: with mbar_wait's record at each of the twenty waits, one copy of each warp's loads and one
+// of the result's reads (129 -> 105 KB), trees of 8 nodes over 4096 rows of 410 tokens went from
+// 285 to 197 us, a prompt of 4096 from 93.5 to 91.2 us.
+__device__ __forceinline__ bool att_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+#pragma unroll 1
+  for (;;) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*abort) return false;
+    if (globaltimer_ns() - t0 > kAttWaitNs) {
+      *abort = site;
+      return false;
+    }
+  }
 }
 
 // What the producer tells the other warps of an item.
@@ -322,9 +347,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   const int tpt = kAttRows / a.G;
 
   // Waits for published item number k; false: no more, or the wait gave up.
-  auto ready = [&](int k, unsigned site) {
+  auto ready = [&](int k, int site) {
     const int e = k % kItemRing;
-    return att_wait(&b_item[e], (k / kItemRing) & 1, abort, a.dbg, site, (unsigned)k) && ring[e].it.y >= 0;
+    return att_wait(&b_item[e], (k / kItemRing) & 1, abort, site) && ring[e].it.y >= 0;
   };
 
   if (warp >= 8) {
@@ -359,7 +384,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         for (int k = 0; !*abort; ++k) {
           const AttnItem it = next;
           const int e = k % kItemRing;
-          if (!att_wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, abort, a.dbg, 200u, (unsigned)k)) break;
+          if (!att_wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, abort, 200)) break;
           int4* p = reinterpret_cast<int4*>(ring + e);
           p[0] = make_int4(it.y, it.h, it.lb, it.t0);
           p[1] = make_int4(it.tend, it.k0, it.klen, it.off);
@@ -372,27 +397,25 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           if (it.y < 0) break;
           fetch();
           if (st.n == 0) continue;
-          if (!att_wait(b_qempty, (sent & 1) ^ 1, abort, a.dbg, 201u, (unsigned)k)) break;
+          if (!att_wait(b_qempty, (sent & 1) ^ 1, abort, 201)) break;
           mbar_expect_tx(b_qfull, st.alt ? qbytes : 2 * qbytes);
           for (int x = 0; x < (st.alt ? 1 : 2); ++x)
             for (int c = 0; c < D / 64; ++c)
               tma_load_5d(smem + L::Q + x * L::TILE + c * 16384, &tmQ, c * 64, 0, it.h, it.t0 + x * tpt, it.lb, b_qfull);
           ++sent;
-          auto load = [&](int j, bool v) {
-            const int s = g % ST;
-            if (!att_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, a.dbg, 202u, (unsigned)g)) return;
+#pragma unroll 1
+          for (int p2 = 0; p2 < 2 * st.n; ++p2) {
+            bool v;
+            const int j = st.tile(st.load(p2, v)), s = g % ST;
+            if (!att_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, 202)) break;
             mbar_expect_tx(&b_full[s], L::TILE);
             const bool d = TREE && j == st.draft;
             const CUtensorMap* tm = d ? (v ? &tmVD : &tmKD) : v ? &tmV : &tmK;
+#pragma unroll
             for (int c = 0; c < D / 64; ++c)
               tma_load_3d(smem + L::RING + s * L::TILE + c * 16384, tm, c * 64, it.y, d ? 0 : it.k0 + j * kAttTok,
                           &b_full[s], pol);
             ++g;
-          };
-          for (int i = 0; i < st.look && i < st.n; ++i) load(st.tile(i), false);
-          for (int i = 0; i < st.n && !*abort; ++i) {
-            load(st.tile(i), true);
-            if (i + st.look < st.n) load(st.tile(i + st.look), false);
           }
         }
         // every issued load must land before the CTA may exit
@@ -410,16 +433,16 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         Place<ST> g;
         uint32_t items = 0, np[2] = {0, 0};  // query tiles and P tiles taken, modulo 2
         bool ok = true;
-        for (int k = 0; ok && ready(k, 203u); ++k) {
+        for (int k = 0; ok && ready(k, 203); ++k) {
           const Steps<TREE> st(ring[k % kItemRing].it);
           if (st.n == 0) {
             mbar_arrive(&b_free[k % kItemRing]);
             continue;
           }
-          ok = att_wait(b_qfull, items, abort, a.dbg, 204u, (unsigned)k);
+          ok = att_wait(b_qfull, items, abort, 204);
           if (!ok) break;
           items ^= 1u;
-          auto full = [&](const Place<ST>& p) { return att_wait(&b_full[p.s], p.phase, abort, a.dbg, 205u, (unsigned)k); };
+          auto full = [&](const Place<ST>& p) { return att_wait(&b_full[p.s], p.phase, abort, 205); };
           auto s_mma = [&](int x, uint32_t qlo, uint32_t stage) {
             const uint32_t klo = k_lo + stage * (L::TILE >> 4);
 #pragma unroll
@@ -433,7 +456,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             const uint32_t vlo = v_lo + stage * (L::TILE >> 4);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              if (!att_wait(&b_p[2 * x + h], np[x], abort, a.dbg, 206u, (unsigned)k)) return false;
+              if (!att_wait(&b_p[2 * x + h], np[x], abort, 206)) return false;
               tc_fence_after();
 #pragma unroll
               for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
@@ -524,20 +547,23 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       // (These warps wait for and release every load, so that a stage's phase cannot pass them by,
       // nor they it: a wait for a parity is sound only one phase away.)
       Place<ST> g;
-      for (int k = 0; __all_sync(0xffffffffu, ready(k, 207u)); ++k) {
+      for (int k = 0; __all_sync(0xffffffffu, ready(k, 207)); ++k) {
         const Steps<TREE> st(ring[k % kItemRing].it);
         int found = 0;
         bool ok = true;
-        auto pass = [&](int i) {  // i >= 0: V of step i, else some K
-          ok = __all_sync(0xffffffffu, ok && att_wait(&b_full[g.s], g.phase, abort, a.dbg, 208u, (unsigned)k));
-          const int mk = ok && i >= 0 ? st.masked(i) : 0;
+#pragma unroll 1
+        for (int p2 = 0; p2 < 2 * st.n; ++p2) {
+          ok = __all_sync(0xffffffffu, att_wait(&b_full[g.s], g.phase, abort, 208));
+          if (!ok) break;
+          bool v;
+          const int i = st.load(p2, v), mk = v ? st.masked(i) : 0;
           if (mk) {
             // the keys that some row must not see
             const int j = st.tile(i);
             int lo = max(0, min(mk & 1 ? st.lowA : kSeesAll, mk & 2 ? st.lowB : kSeesAll) - j * kAttTok), hi = kAttTok;
             if (TREE && j == st.draft) lo = 0, hi = a.nodes;
             uint32_t acc[4] = {};
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < D / 64; ++c) {
               const uint4* vt = reinterpret_cast<const uint4*>(smem + L::RING + g.s * L::TILE + c * 16384);
 #pragma unroll 4
@@ -552,13 +578,8 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             if (__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7fff7fffu) != 0u)) found |= mk;
           }
           __syncwarp();
-          if (ok && lane == 0) mbar_arrive(&b_empty[g.s]);
+          if (lane == 0) mbar_arrive(&b_empty[g.s]);
           ++g;
-        };
-        for (int i = 0; i < st.look && i < st.n; ++i) pass(-1);
-        for (int i = 0; i < st.n && ok; ++i) {
-          pass(i);
-          if (i + st.look < st.n) pass(-1);
         }
         if (!ok) break;
         if (lane == 0) {
@@ -580,7 +601,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     const float c = a.c, grow = 8.f / c;
     const int row_t = row / a.G, row_g = row % a.G;
     uint32_t ns = 0, no = 0, oo = 0, nx = 0;  // S tiles, results (oo: the other's) and exchanges so far, modulo 2
-    for (int k = 0; __all_sync(0xffffffffu, ready(k, 209u)); ++k) {
+    for (int k = 0; __all_sync(0xffffffffu, ready(k, 209)); ++k) {
       const AttnItem& it = ring[k % kItemRing].it;  // (not kept in registers through the steps)
       const int4 of = ring[k % kItemRing].of[X];
       const int alt = it.alt, steps = of.z, low = of.w, klen = it.klen;
@@ -599,7 +620,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       const int jstep = TREE ? alt + 1 : -1 - alt;
 #pragma unroll 1
       for (int i = 0; i < steps; ++i, j += jstep) {
-        att_wait(&b_s[X], ns, abort, a.dbg, 210u + X, (unsigned)k);
+        att_wait(&b_s[X], ns, abort, 210 + X);
         ns ^= 1u;
         if (busy) {
           tc_fence_after();
@@ -699,7 +720,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
 
       // ---------------------------------------------------------- the item's result
       // (all that does not need O goes before the wait for it)
-      att_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, a.dbg, 214u, (unsigned)k);
+      att_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, 214);
       const int found = flags[2 * (k % kItemRing)] | flags[2 * (k % kItemRing) + 1];
       const bool bad = alt ? found != 0 : (found >> X & 1) != 0;
       // of two results over the same rows, each warpgroup joins half the dims
@@ -709,7 +730,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         xch[X * 128 + row] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(&b_x[0]);
-        att_wait(&b_x[0], nx, abort, a.dbg, 215u, (unsigned)k);
+        att_wait(&b_x[0], nx, abort, 215);
         const float2 y = xch[(X ^ 1) * 128 + row];
         const float mm = fmaxf(m, y.x);
         other = ring[k % kItemRing].of[X ^ 1].z;
@@ -754,11 +775,11 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         fy *= inv;
       }
       if (steps) {
-        att_wait(&b_o[X], no, abort, a.dbg, 212u + X, (unsigned)k);
+        att_wait(&b_o[X], no, abort, 212 + X);
         no ^= 1u;
       }
       // (the other's products: it has passed its earlier results, as its part of the exchange says)
-      if (other) att_wait(&b_o[X ^ 1], oo, abort, a.dbg, 213u, (unsigned)k);
+      if (other) att_wait(&b_o[X ^ 1], oo, abort, 213);
       oo ^= ring[k % kItemRing].of[X ^ 1].z ? 1u : 0u;
       tc_fence_after();
       if (bad) {
@@ -816,35 +837,28 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             }
           }
         };
-        if (slot >= 0) {
+        // 128 bytes of each row at a time: 64 dims, or 32 of a partial result (or 32 that are all there
+        // are: each row's second half is then written by no lane)
+        const uint32_t both = slot < 0 && d1 - d0 < 64 && (lane & 4) ? 0u : on;
 #pragma unroll 1
-          for (int d = d0; d < d1; d += 32) {
-            float o[32];
-            dims(d, o);
+        for (int d = d0; d < d1; d += 32) {
+          float o[32];
+          dims(d, o);
+          if (slot >= 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               buf[lane * 8 + (e ^ (lane & 7))] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
                                                             __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
-            flush_rows(buf, to, on, d * 4);
-          }
-        } else {
-          // 64 dims at a time (of 32 only, each row's second half is written by no lane)
-          const uint32_t half = d1 - d0 < 64 && (lane & 4) ? 0u : on;
-#pragma unroll 1
-          for (int d = d0; d < d1; d += 64) {
+          } else {
+            const int h = (d - d0) >> 3 & 4;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (d + h * 32 >= d1) break;
-              float o[32];
-              dims(d + h * 32, o);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                buf[lane * 8 + ((h * 4 + e) ^ (lane & 7))] =
-                    make_uint4(T::pack(o[8 * e], o[8 * e + 1]), T::pack(o[8 * e + 2], o[8 * e + 3]),
-                               T::pack(o[8 * e + 4], o[8 * e + 5]), T::pack(o[8 * e + 6], o[8 * e + 7]));
-            }
-            flush_rows(buf, to, half, d * 2);
+            for (int e = 0; e < 4; ++e)
+              buf[lane * 8 + ((h + e) ^ (lane & 7))] =
+                  make_uint4(T::pack(o[8 * e], o[8 * e + 1]), T::pack(o[8 * e + 2], o[8 * e + 3]),
+                             T::pack(o[8 * e + 4], o[8 * e + 5]), T::pack(o[8 * e + 6], o[8 * e + 7]));
+            if (!h && d + 32 < d1) continue;
           }
+          flush_rows(buf, to, both, slot >= 0 ? d * 4 : (d & ~63) * 2 + (d1 - d0 < 64 ? d0 % 64 * 2 : 0));
         }
       }
       tc_fence_before();
@@ -852,7 +866,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       if (alt) {
         // the other warpgroup has read this one's O and statistics before they are written again
         if (lane == 0) mbar_arrive(&b_x[1]);
-        att_wait(&b_x[1], nx, abort, a.dbg, 216u, (unsigned)k);
+        att_wait(&b_x[1], nx, abort, 216);
         nx ^= 1u;
       }
       if (lane == 0) mbar_arrive(&b_free[k % kItemRing]);
@@ -863,7 +877,10 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, kAttCols);
   }
-  if (threadIdx.x == 0 && *abort) atomicOr(a.status, kStatusTimeout);
+  if (threadIdx.x == 0 && *abort) {
+    record_timeout(a.dbg, (unsigned)*abort, 0u, 0u);
+    atomicOr(a.status, kStatusTimeout);
+  }
 }
 
 // Joins the partial results of the parts of one item, in order: block x an item, y 32 of its rows, a

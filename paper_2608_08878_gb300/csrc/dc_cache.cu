@@ -1075,7 +1075,7 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   const char* why = nullptr;
   {
     Phase ph(h, DC_PHASE_FULL, slots ? 2 : 1);
-    e = dc::launch_tree(a, p.d, p.stride, h->stream, &why);
+    e = dc::launch_tree(a, p.d, h->stream, &why);
   }
   if (why) return fail(h, DC_ERR_INVALID_ARG, why);
   if (e != cudaSuccess) return cuda_fail(h, e, "tree attention");

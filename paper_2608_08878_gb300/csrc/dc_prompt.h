@@ -22,10 +22,9 @@ bool att_map_kv(CUtensorMap* m, bool bf16, const void* base, int D, long long ys
 
 // Attention of drafted trees over the rows of a cache (AttnArgs' tree fields), D 64 or
 // 128. tree_plan sets how the work is divided, and returns the partial results' slots (-1: too
-// much work to count);
-// launch_tree needs a.part and a.part_ml for them.
+// much work to count); launch_tree needs a.part and a.part_ml for them. *why on a map that the
+// driver rejects.
 long long tree_plan(AttnArgs* a, int num_sms);
-// `tokens`: the row stride in slots. *why on a map that the driver rejects.
-cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, cudaStream_t s, const char** why);
+cudaError_t launch_tree(const AttnArgs& a, int D, cudaStream_t s, const char** why);
 
 }  // namespace dc

@@ -27,8 +27,9 @@ long long tree_plan(AttnArgs* a, int num_sms) {
   return cut ? 2ll * grid : 0;
 }
 
-cudaError_t launch_tree(const AttnArgs& a, int D, long long tokens, cudaStream_t s, const char** why) {
+cudaError_t launch_tree(const AttnArgs& a, int D, cudaStream_t s, const char** why) {
   AttMaps m;
+  const long long tokens = std::max(1, a.n);  // (slots beyond are not read: their places are filled with zeros)
   const bool ok = att_map_q(&m.q, true, a, D, a.nodes, a.rows / a.kvh) &&
                   att_map_kv(&m.k, true, a.k, D, a.rows, a.k_y, tokens, a.k_t) &&
                   att_map_kv(&m.v, true, a.v, D, a.rows, a.v_y, tokens, a.v_t) &&
