@@ -443,10 +443,10 @@ def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps:
         s = here.__enter__()
     try:
         if q_out is None:
-            q_out = torch.empty((T, hq, d), dtype=dtype, device=q.device)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             to_q = q_out.data_ptr(), hq * d, d
         if k_out is None:
-            k_out = torch.empty((T, hk, d), dtype=dtype, device=q.device)
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
             to_k = k_out.data_ptr(), hk * d, d
         L = lib()
         st = L.dc_norm_rotate(dc_rotate_args(T, hq, hk, d, 2 * pairs, kind, 1 if norm else 0, 1 if interleaved else 0, eps,
@@ -525,7 +525,7 @@ class PromptPlan:
             s = here.__enter__()
         try:
             if out is None:
-                out = torch.empty(q.shape, dtype=dtype, device=q.device)
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
             need = self.workspace_bytes
             work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
@@ -707,10 +707,10 @@ class DistillCache:
         pv = _arg(v_draft, "v_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         if out is None:
             if _raw_stream(self.device) == self.stream.cuda_stream:
-                out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
             else:  # (what the cache's stream writes belongs to that stream)
                 with torch.cuda.stream(self.stream):
-                    out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+                    out = torch.empty_like(q, memory_format=torch.contiguous_format)
         po = _arg(out, "out", torch.bfloat16, n * self.q_heads, device=self.device)
         self._check(lib().dc_tree_attend(self._h, pq, pk, pv, pp, T, po))
         return out
