@@ -42,7 +42,7 @@ struct AttnArgs {
   int prows;
   long long out_len, part_rows;  // debug builds: elements of out, rows of part
   // trees
-  int n, nodes, batch, rows, pairs, tiles, grid, per, extra;
+  int n, nodes, batch, rows, pairs, tiles, grid, line, ctas, per, extra;
   const int* rowlen;         // each row's length, or null (n)
   const int* parents;        // [batch][nodes]
   unsigned* status;

@@ -14,13 +14,14 @@ long long tree_plan(AttnArgs* a, int num_sms) {
   a->tiles = (a->n + kAttTok - 1) / kAttTok + 1;
   const long long total = (long long)a->n_items * a->tiles;  // (8 million at most in this GPU's memory)
   if (total >= 1ll << 30) return -1;
-  // CTAs: every SM an equal share of all key tiles, but at least 2 tiles; or, of few items,
+  // CTAs: every SM an equal share of a line's key tiles, but at least 2 tiles; or, of few items,
   // one each, where the items are so short that parts would not pay for the merge (about 6 tiles).
-  int grid = (int)std::min<long long>(num_sms, std::max<long long>(1, total / 2));
-  if (a->n_items <= num_sms && (a->tiles <= 8 || a->n_items == num_sms)) grid = a->n_items;
-  a->grid = grid;
-  a->per = (int)(total / grid);
-  a->extra = (int)(total % grid);
+  a->line = a->rows * a->tiles;
+  a->ctas = std::min(num_sms / a->pairs, std::max(1, a->line / 2));
+  if (a->n_items <= num_sms && (a->tiles <= 8 || a->n_items == num_sms)) a->ctas = a->rows;
+  a->per = a->line / a->ctas;
+  a->extra = a->line % a->ctas;
+  const int grid = a->grid = a->ctas * a->pairs;
   bool cut = false;
   for (int b = 1; b < grid && !cut; ++b) cut = tree_from(*a, b) % a->tiles != 0;
   a->n_merges = cut ? grid - 1 : 0;
