@@ -244,3 +244,19 @@ def test_row_offsets_past_32_bits():
         o, _, tol, _ = attention64(q[0, 0, :, g], torch.cat([k[0, 0, g], kd[0, 0, g]]), torch.cat([v[0, 0, g], vd[0, 0, g]]),
                                    seen, d ** -0.5)
         check(out[0, 0, :, g], o, tol)
+
+
+@pytest.mark.parametrize("layers,batch,kvh,group,d,n,T", [
+    (10, 4, 4, 8, 64, 515, 64), (7, 3, 4, 8, 128, 300, 96), (5, 4, 8, 8, 64, 129, 128), (19, 1, 8, 4, 128, 900, 100),
+    (1, 1, 8, 8, 128, 5000, 70), (38, 2, 1, 8, 64, 1100, 33)])
+def test_several_pairs_of_query_tiles(layers, batch, kvh, group, d, n, T):
+    run(layers, batch, kvh, group, d, n, T)
+
+
+def test_random_shapes():
+    import random
+    r = random.Random(5)
+    for i in range(30):
+        group = r.choice([1, 2, 4, 8])
+        run(r.choice([1, 2, 5]), r.choice([1, 3, 8]), r.choice([1, 2, 8]), group, r.choice([64, 128]), int(2 ** r.uniform(0, 11)),
+            min(128, int(2 ** r.uniform(0, 7.2))), kind=r.choice(["random", "chain", "flat", "holes"]), seed=i)
