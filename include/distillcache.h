@@ -265,7 +265,8 @@ dc_status dc_full_decode(dc_cache* h, const void* q, float* out);
  * be empty. Rows of different lengths (dc_set_row_budgets) are taken. A key or value
  * that a node does not see leaves its output alone, whatever it holds. Launches count
  * as DC_PHASE_FULL. The first call that divides rows among CTAs allocates (DC_ERR_OOM; DC_ERR_STATE
- * in a stream capture, which needs one call before it). */
+ * in a stream capture, which needs one call before it). A captured call replays over as many cached
+ * tokens as there were when it was captured: capture anew when the cache's length has changed. */
 dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const void* v_draft,
                          const int* parents, int nodes, void* out);
 

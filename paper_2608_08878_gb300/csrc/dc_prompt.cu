@@ -328,6 +328,7 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   if (x.workspace_bytes < p->workspace() || (p->workspace() && (!x.workspace || (uintptr_t)x.workspace & 15)))
     return prompt_fail(DC_ERR_INVALID_ARG, "the workspace must hold dc_prompt_workspace bytes, 16-byte aligned");
   if (at & 15) return prompt_fail(DC_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+  if ((uintptr_t)x.lse & 3) return prompt_fail(DC_ERR_INVALID_ARG, "lse must be 4-byte aligned");
   int dev = -1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return prompt_cuda(e, "cudaGetDevice");

@@ -270,3 +270,26 @@ def test_random_shapes():
         k_lens = [max(0, x + r.choice([0, 0, -2, int(2 ** r.uniform(0, 11))])) for x in q_lens]
         run(q_lens, r.choice([1, 2, 3, 8]), r.choice([1, 2, 3, 4, 5, 8]), r.choice([64, 128]), r.choice([BF, HF]), k_lens,
             r.random() < 0.8, seed=i)
+
+
+def test_lse_off_4_bytes_is_refused():
+    import ctypes as C
+    q, k, v = inputs([8], [8], 2, 2, 64, BF)
+    plan, out, lse = dc.PromptPlan([8], 2, 64, q_heads=4), torch.empty_like(q), torch.empty(64, device="cuda")
+    for at, status in ((2, dc.DC_ERR_INVALID_ARG), (4, dc.DC_OK)):
+        a = dc.dc_prompt_args(0, 0.125, q.data_ptr(), k.data_ptr(), v.data_ptr(), 256, 64, 128, 64, 128, 64, out.data_ptr(),
+                              lse.data_ptr() + at, None, 0)
+        assert dc.lib().dc_prompt_attend(plan._p, C.byref(a), None) == status
+    plan.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("step", [5.0, 9.0, 14.0, 14.9, 15.5, 23.5, 25.0, 70.0])
+def test_maxima_that_rise_by_powers_of_two(step, dtype):
+    """Every 128 keys the scores rise by a factor of 2^step in weight: references that stay, and ones that move."""
+    for sign in (1, -1):
+        q, k, v = inputs([900], [900], 1, 4, 64, dtype)
+        q[..., 0] = 8.0
+        k[:, 0, 0] = (sign * step * math.log(2) * (torch.arange(900, device="cuda") // 128)).to(dtype)
+        out, lse = dc.PromptPlan([900], 1, 64, q_heads=4).attend(q, k, v, with_lse=True)
+        compare(out, lse, q, k, v, [900], [900])
