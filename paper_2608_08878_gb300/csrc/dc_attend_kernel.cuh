@@ -39,8 +39,9 @@
 // (2390 without any softmax): the tensor pipe and the hand-over between the halves. One sequence
 // of 32768 tokens, 32 query heads on 8 KV heads: 5.4 ms, 1.63 PFLOP/s; 4096 tokens: 91 us; trees of 16
 // nodes over 2048 rows of 8192 tokens read the cache at 7.2 TB/s (1.18 ms). At D 64 a step has 1024
-// cycles of products and takes 2650 all the same: the chain S, softmax, P, O, S of each half, of which
-// only two fit into TMEM (a quarter of the exponentials as polynomials beside the others: 9% slower).
+// cycles of products and takes 2650 all the same: there the softmax of two warps per scheduler bounds it (4096
+// tokens, 64 heads: 149 us; without exponentials 120, without maxima 139. A quarter of the
+// exponentials as polynomials: 162. A third S in TMEM, so that no warp waits for one: 148-154).
 //
 // Results go through shared memory, 128 bytes of each of a warp's 32 rows at a time, so that they
 // leave together (a thread writing its own row cost 5000 to 7000 cycles an item).
