@@ -43,6 +43,7 @@ struct AttnArgs {
   long long out_len, part_rows;  // debug builds: elements of out, rows of part
   // trees
   int n, nodes, batch, rows, pairs, tiles, grid, line, ctas, per, extra;
+  int two;  // whether items are two rows of one query tile each
   const int* rowlen;         // each row's length, or null (n)
   const int* parents;        // [batch][nodes]
   unsigned* status;
@@ -57,7 +58,7 @@ struct AttnItem {
   int off;        // query token t sees keys [0, min(klen, t + off)); kSeesAll: all
   int j0, j1;     // key tiles
   int slot;       // where a part of the keys leaves its partial result; -1: all keys
-  int alt;        // one tile of query rows only
+  int alt;        // 1: one tile of query rows only; 2 (trees): one tile of row y and one of row y + 1
   int eA, eB;     // key tiles that A's and B's rows see: below these
   int lowA, lowB; // what A's and B's first row sees, the least of their rows
 };

@@ -28,7 +28,8 @@
 //
 // Items of one tile of queries (single tokens, small trees, short sequences) give their key
 // tiles to A and B in turn, both on the same queries, and join the two results at the end:
-// the pipeline is the same.
+// the pipeline is the same. Small trees over many short rows take two rows at a time instead, A one
+// and B the other, with nothing to join.
 //
 // A masked key has weight 0, but 0 times a value that is not finite is NaN: warps 10 and 11 look
 // over the values that some row of the tile must not see, in shared memory, before their stage
@@ -115,20 +116,20 @@ __device__ __forceinline__ AttnItem tree_item(const AttnArgs& a, int b, int at, 
   const int tpt = kAttRows / a.G, i = at / a.tiles, j0 = at - i * a.tiles;
   const int j1 = min(a.tiles, j0 + end - at);
   AttnItem it;
-  it.y = i % a.rows;
+  it.y = a.two ? 2 * i : i % a.rows;
   it.lb = it.y / a.kvh;
   it.h = it.y % a.kvh;
-  it.t0 = i / a.rows * 2 * tpt;
+  it.t0 = a.two ? 0 : i / a.rows * 2 * tpt;
   it.tend = a.nodes;
   it.k0 = 0;
   it.klen = a.rowlen ? __ldg(a.rowlen + it.y) : a.n;
   it.off = kSeesAll;
   const int own = (it.klen + kAttTok - 1) / kAttTok + 1;
-  it.j0 = min(j0, own);
-  it.j1 = min(j1, own);
+  it.j0 = a.two ? 0 : min(j0, own);
+  it.j1 = a.two ? own : min(j1, own);
   // a CTA has at most two parts of items: the end of one, then the start of another
   it.slot = j0 == 0 && j1 == a.tiles ? -1 : 2 * b + (j0 == 0 ? 1 : 0);
-  it.alt = it.tend - it.t0 <= tpt;
+  it.alt = a.two && it.y + 1 < a.rows ? 2 : it.tend - it.t0 <= tpt;
   it.eA = it.eB = it.j1;
   it.lowA = it.lowB = it.klen;
   return it;
@@ -140,11 +141,11 @@ template <bool TREE>
 struct Steps {
   int n, j0, j1, alt, look, skipA, skipB, lowA, lowB, draft;
   __device__ __forceinline__ Steps(const AttnItem& it)
-      : n(it.j1 - it.j0), j0(it.j0), j1(it.j1), alt(it.alt), look(it.alt ? 2 : 1), skipA(max(0, it.j1 - it.eA)),
+      : n((it.j1 - it.j0) << (it.alt == 2)), j0(it.j0), j1(it.j1), alt(it.alt), look(it.alt ? 2 : 1), skipA(max(0, it.j1 - it.eA)),
         skipB(max(0, it.j1 - it.eB)), lowA(it.lowA), lowB(it.lowB),
         draft(TREE ? (it.klen + kAttTok - 1) / kAttTok : -1) {}
   // the tiles that may be masked come first in prompts, last in trees
-  __device__ __forceinline__ int tile(int i) const { return TREE ? j0 + i : j1 - 1 - i; }
+  __device__ __forceinline__ int tile(int i) const { return TREE ? j0 + (i >> (alt == 2)) : j1 - 1 - i; }
   // whether some row of tile A (x = 0) or B must not see some key of step i's tile
   __device__ __forceinline__ bool masked(int i, int x) const {
     const int j = tile(i);
@@ -410,28 +411,30 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           p[3] = make_int4(it.eA, it.eB, it.lowA, it.lowB);
           const Steps<TREE> st(it);
           p[4] = make_int4(it.t0, st.alt ? 0 : st.skipA, st.count(0), it.lowA);
-          p[5] = make_int4(st.alt ? it.t0 : it.t0 + tpt, st.alt ? 1 : st.skipB, st.count(1), it.lowB);
+          p[5] = make_int4(st.alt ? it.t0 : it.t0 + tpt, st.alt ? st.alt & 1 : st.skipB, st.count(1), it.lowB);
           mbar_arrive(&b_item[e]);
           if (it.y < 0) break;
           fetch();
           if (st.n == 0) continue;
           if (!att_wait(b_qempty, (sent & 1) ^ 1, abort, 201)) break;
-          mbar_expect_tx(b_qfull, st.alt ? qbytes : 2 * qbytes);
-          for (int x = 0; x < (st.alt ? 1 : 2); ++x)
+          const bool two = TREE && st.alt == 2;
+          mbar_expect_tx(b_qfull, st.alt == 1 ? qbytes : 2 * qbytes);
+          for (int x = 0; x < (st.alt == 1 ? 1 : 2); ++x)
             for (int c = 0; c < D / 64; ++c)
-              tma_load_5d(smem + L::Q + x * L::TILE + c * 16384, &tmQ, c * 64, 0, it.h, it.t0 + x * tpt, it.lb, b_qfull);
+              tma_load_5d(smem + L::Q + x * L::TILE + c * 16384, &tmQ, c * 64, 0, two ? (it.y + x) % a.kvh : it.h,
+                          two ? 0 : it.t0 + x * tpt, two ? (it.y + x) / a.kvh : it.lb, b_qfull);
           ++sent;
 #pragma unroll 1
           for (int p2 = 0; p2 < 2 * st.n; ++p2) {
             bool v;
-            const int j = st.tile(st.load(p2, v)), s = g % ST;
+            const int i = st.load(p2, v), j = st.tile(i), s = g % ST;
             if (!att_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, 202)) break;
             mbar_expect_tx(&b_full[s], L::TILE);
             const bool d = TREE && j == st.draft;
             const CUtensorMap* tm = d ? (v ? &tmVD : &tmKD) : v ? &tmV : &tmK;
 #pragma unroll
             for (int c = 0; c < D / 64; ++c)
-              tma_load_3d(smem + L::RING + s * L::TILE + c * 16384, tm, c * 64, it.y, d ? 0 : it.k0 + j * kAttTok,
+              tma_load_3d(smem + L::RING + s * L::TILE + c * 16384, tm, c * 64, it.y + (two ? i & 1 : 0), d ? 0 : it.k0 + j * kAttTok,
                           &b_full[s], pol);
             ++g;
           }
@@ -487,12 +490,13 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           const int n = st.n;
           if (st.alt) {
             // A: steps 0, 2, ..., B: 1, 3, ...; S of a step goes out behind O of the one two before
+            const uint32_t q1 = st.alt == 2 ? q_lo + (L::TILE >> 4) : q_lo;
             for (int i = 0; i < 2 && i < n; ++i) {
               ok = ok && full(g);
               if (!ok) break;
               tc_fence_after();
               if (i == 0) s_mma(0, q_lo, g.s);
-              else s_mma(1, q_lo, g.s);
+              else s_mma(1, q1, g.s);
               mma_commit(&b_empty[g.s]);
               ++g;
             }
@@ -506,7 +510,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
               if (i + 2 < n) {
                 if (!full(g)) return false;
                 tc_fence_after();
-                s_mma(x, q_lo, g.s);
+                s_mma(x, x ? q1 : q_lo, g.s);
                 mma_commit(&b_empty[g.s]);
                 ++g;
                 if (i + 3 == n) mma_commit(b_qempty);
@@ -622,7 +626,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     for (int k = 0; __all_sync(0xffffffffu, ready(k, 209)); ++k) {
       const AttnItem& it = ring[k % kItemRing].it;  // (not kept in registers through the steps)
       const int4 of = ring[k % kItemRing].of[X];
-      const int alt = it.alt, steps = of.z, low = of.w, klen = it.klen;
+      const int alt = it.alt == 1, steps = of.z, low = of.w, klen = it.klen;
+      const bool two = TREE && it.alt == 2;
+      const int y = two ? it.y + X : it.y, lb = two ? y / a.kvh : it.lb;
       const int draft = TREE ? (klen + kAttTok - 1) / kAttTok : -1;
       const int t = of.x + row_t;
       const bool valid = row < tpt * a.G && t < it.tend;
@@ -631,7 +637,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       const bool drafts = TREE && it.j0 <= draft && draft < it.j1;
       uint32_t nodes[4] = {};
       bool sees = TREE || lim > 0;
-      if (drafts && valid) sees = tree_mask(a.parents + (long long)(it.lb % a.batch) * a.nodes, t, nodes);
+      if (drafts && valid) sees = tree_mask(a.parents + (long long)(lb % a.batch) * a.nodes, t, nodes);
 
       float m = -INFINITY, l = 0.f;
       int j = TREE ? it.j0 + of.y : it.j1 - 1 - of.y;
@@ -765,7 +771,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           x.out = reinterpret_cast<uint8_t*>(a.part + ((long long)slot * a.prows + r) * D);
           x.part_ml = a.part_ml + ((long long)slot * a.prows + r);
         } else {
-          x.out = reinterpret_cast<uint8_t*>(a.out + it.lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h);
+          x.out = reinterpret_cast<uint8_t*>(a.out + lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h);
           x.part_ml = nullptr;
         }
         return x;
@@ -773,9 +779,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       // (debug builds: whether the row's place lies within the output or the partial results)
       auto fits = [&](int tok, int hd, int r) {
         return slot >= 0 ? DC_INB(a, (long long)slot * a.prows + r, a.part_rows, 320)
-                         : DC_INB(a, it.lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h + D - 1, a.out_len, 321);
+                         : DC_INB(a, lb * a.o_lb + (long long)tok * a.o_t + hd * a.o_h + D - 1, a.out_len, 321);
       };
-      const int head = it.h * a.G + row_g, prow = (alt ? 0 : X * 128) + row;
+      const int head = (two ? y % a.kvh : it.h) * a.G + row_g, prow = (alt ? 0 : X * 128) + row;
       RowOut ro = place(t, head, prow);
       ro.sees = sees;
       const bool writes = valid && fits(t, head, prow);
@@ -815,9 +821,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             x.sees = __shfl_sync(0xffffffffu, (int)sees, rr);
             const int from = it.j0 * kAttTok, to = x.sees ? min(see, it.j1 * kAttTok) : from;
             float o[D / 32], mm, ll;
-            const long long dr = (long long)it.y * a.nodes * D;
-            attend_row<T, D>(a, a.q + it.lb * a.q_lb + (long long)tok * a.q_t + hd * a.q_h,
-                             a.k + it.k0 * a.k_t + it.y * a.k_y, a.v + it.k0 * a.v_t + it.y * a.v_y, a.kd + dr, a.vd + dr,
+            const long long dr = (long long)y * a.nodes * D;
+            attend_row<T, D>(a, a.q + lb * a.q_lb + (long long)tok * a.q_t + hd * a.q_h,
+                             a.k + it.k0 * a.k_t + y * a.k_y, a.v + it.k0 * a.v_t + y * a.v_y, a.kd + dr, a.vd + dr,
                              from, to, drafts && x.sees ? w : nullptr, mm, ll, o);
             if (lane == 0) x.stats(a, mm, ll);
             const float inv = x.sees ? 1.f / ll : 0.f;

@@ -1047,7 +1047,7 @@ dc_status dc_tree_attend(dc_cache* h, const void* q, const void* k_draft, const 
   a.parents = parents;
   a.status = p.status;
   a.dbg = p.dbg;
-  const long long slots = dc::tree_plan(&a, h->num_sms);
+  const long long slots = dc::tree_plan(&a, p.d, h->num_sms);
   if (slots < 0) return fail(h, DC_ERR_INVALID_ARG, "too many tokens");
   if (slots) {
     // the partial results of rows in parts: one buffer for any call (two parts a CTA at most), made by

@@ -24,7 +24,7 @@ bool att_map_kv(CUtensorMap* m, bool bf16, const void* base, int D, long long ys
 // 128. tree_plan sets how the work is divided, and returns the partial results' slots (-1: too
 // much work to count); launch_tree needs a.part and a.part_ml for them. *why on a map that the
 // driver rejects.
-long long tree_plan(AttnArgs* a, int num_sms);
+long long tree_plan(AttnArgs* a, int D, int num_sms);
 cudaError_t launch_tree(const AttnArgs& a, int D, cudaStream_t s, const char** why);
 
 }  // namespace dc

@@ -6,7 +6,7 @@
 
 namespace dc {
 
-long long tree_plan(AttnArgs* a, int num_sms) {
+long long tree_plan(AttnArgs* a, int D, int num_sms) {
   const int tpt = kAttRows / a->G;
   a->pairs = (a->nodes + 2 * tpt - 1) / (2 * tpt);
   a->prows = a->nodes <= tpt ? a->nodes * a->G : 256;
@@ -19,6 +19,17 @@ long long tree_plan(AttnArgs* a, int num_sms) {
   a->line = a->rows * a->tiles;
   a->ctas = std::min(num_sms / a->pairs, std::max(1, a->line / 2));
   if (a->n_items <= num_sms && (a->tiles <= 8 || a->n_items == num_sms)) a->ctas = a->rows;
+  // More rows than SMs, short ones of one query tile: two whole rows an item, so that nothing is joined and
+  // each half has its own chain of steps. Trees of 8 nodes, one row an item -> two, us: 256 rows x 410 tokens
+  // of 128 dims 28 -> 16, 4096 x 410 206 -> 185, 4096 x 640 232 -> 235, 4096 x 1000 331 -> 342; of 64 dims 4096 x 410
+  // 193 -> 133, 4096 x 1000 248 -> 208. Long rows read at the same rate either way, and parts of equal size
+  // balance better than whole rows.
+  a->two = a->rows > num_sms && a->nodes <= tpt && !a->rowlen && a->tiles * D <= 640;
+  if (a->two) {
+    a->tiles = 1;  // (a place is an item)
+    a->line = (a->rows + 1) / 2;
+    a->ctas = std::min(num_sms, a->line);
+  }
   a->per = a->line / a->ctas;
   a->extra = a->line % a->ctas;
   const int grid = a->grid = a->ctas * a->pairs;

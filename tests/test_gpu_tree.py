@@ -260,3 +260,24 @@ def test_random_shapes():
         group = r.choice([1, 2, 4, 8])
         run(r.choice([1, 2, 5]), r.choice([1, 3, 8]), r.choice([1, 2, 8]), group, r.choice([64, 128]), int(2 ** r.uniform(0, 11)),
             min(128, int(2 ** r.uniform(0, 7.2))), kind=r.choice(["random", "chain", "flat", "holes"]), seed=i)
+
+
+@pytest.mark.parametrize("layers,batch,kvh,group,d,n,T,kind", [
+    (5, 4, 8, 4, 128, 410, 8, "random"), (3, 7, 8, 4, 64, 1000, 32, "holes"), (1, 153, 1, 8, 64, 130, 16, "random"),
+    (9, 39, 1, 2, 128, 1, 5, "chain"), (40, 2, 4, 1, 128, 511, 100, "random"), (2, 50, 2, 4, 64, 0, 3, "flat"),
+    (32, 8, 2, 4, 128, 513, 1, "chain"), (1, 155, 2, 4, 128, 300, 7, "unused")])
+def test_many_short_rows(layers, batch, kvh, group, d, n, T, kind):
+    run(layers, batch, kvh, group, d, n, T, kind=kind)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_a_node_does_not_see_in_many_short_rows(bad):
+    for d, rows in ((64, (3, 53, 1)), (128, (5, 8, 4))):
+        cache, (q, kd, vd, parents) = make(*rows, 4, d, 200, 20)
+        ref = cache.tree_attend(q, kd, vd, parents)
+        compare(cache, (q, kd, vd, parents), ref)
+        kd[:, :, :, 19], vd[:, :, :, 19] = bad, bad  # (no node follows the last one)
+        out = cache.tree_attend(q, kd, vd, parents)
+        cache.sync()
+        assert float((out[:, :, :19].float() - ref[:, :, :19].float()).abs().max()) <= 2.0 ** -7 * float(vd[:, :, :, :19].abs().max())
+        assert not bool(torch.isfinite(out[:, :, 19].float()).all(-1).any())
