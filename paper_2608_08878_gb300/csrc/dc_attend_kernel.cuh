@@ -836,6 +836,8 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         }
       } else if (busy) {
         const int d0 = alt ? X * (D / 2) : 0, d1 = alt ? d0 + D / 2 : D;
+        // (an unused node's O holds what its query made of the cached tokens: NaN, of a query that is)
+        const bool blank = __any_sync(0xffffffffu, !sees);
         // 32 dims of this row's result
         auto dims = [&](int d, float (&o)[32]) {
           if (steps) {
@@ -859,6 +861,10 @@ __global__ void __launch_bounds__(kAttThreads, 1)
               o[e] = x.x;
               o[e + 1] = x.y;
             }
+          }
+          if (blank) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = sees ? o[e] : 0.f;
           }
         };
         // 128 bytes of each row at a time: 64 dims, or 32 of a partial result (or 32 that are all there

@@ -281,3 +281,22 @@ def test_what_a_node_does_not_see_in_many_short_rows(bad):
         cache.sync()
         assert float((out[:, :, :19].float() - ref[:, :, :19].float()).abs().max()) <= 2.0 ** -7 * float(vd[:, :, :, :19].abs().max())
         assert not bool(torch.isfinite(out[:, :, 19].float()).all(-1).any())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("rows,group,d,n,T", [
+    ((1, 2, 2), 4, 128, 300, 6), ((1, 2, 2), 8, 64, 300, 100), ((1, 3, 1), 1, 128, 0, 9),  # one item a row or two
+    ((3, 53, 1), 4, 64, 200, 6),                                                           # two rows an item
+    ((1, 1, 2), 4, 128, 5000, 6), ((1, 1, 1), 8, 64, 3000, 70)])                           # rows in parts
+def test_queries_of_unused_nodes_may_hold_anything(rows, group, d, n, T, bad):
+    """An unused node's output is 0 and no other node's changes, whatever its query holds."""
+    cache, (q, kd, vd, parents) = make(*rows, group, d, n, T, kind="chain")
+    parents[:, T // 2] = -7     # (and so is all of the chain behind it)
+    parents[:, T // 2 + 1] = 0  # but for this node and what follows it
+    want = cache.tree_attend(q, kd, vd, parents)
+    compare(cache, (q, kd, vd, parents), want)
+    q[:, :, T // 2] = bad
+    out = cache.tree_attend(q, kd, vd, parents)
+    cache.sync()
+    assert bool((out[:, :, T // 2] == 0).all())
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
