@@ -406,7 +406,8 @@ typedef struct dc_prompt_plan dc_prompt_plan;
  * chunk or a chat turn has more keys, a single token one query; a query with no key
  * (k_len < q_len) gets output 0. causal 0: every query sees every key. head_dim 64 or
  * 128, q_heads = kv_heads times 1 to 128, lengths >= 0. Allocates on the current
- * device and synchronises. */
+ * device and waits for its own upload (not for other work): the plan may be used on any
+ * stream at once. */
 dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int q_heads, int kv_heads,
                                 int head_dim, int causal, dc_prompt_plan** out);
 

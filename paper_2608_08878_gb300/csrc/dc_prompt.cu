@@ -71,6 +71,19 @@ dc_status prompt_cuda(cudaError_t e, const char* what) {
 
 constexpr unsigned kPlanMagic = 0x44435050u;  // "DCPP"
 
+// Copies to the device and waits until it is there, whatever stream the next call is on. (cudaMemcpy may return once
+// pageable memory is staged, and orders the rest on the legacy stream only, which a non-blocking stream does not wait
+// for; and it waits for all that the legacy stream is busy with. A stream of its own does neither.)
+cudaError_t upload_now(void* dst, const void* src, size_t bytes) {
+  cudaStream_t s = nullptr;
+  cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+  if (e != cudaSuccess) return e;
+  e = cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, s);
+  const cudaError_t done = cudaStreamSynchronize(s);
+  cudaStreamDestroy(s);
+  return e != cudaSuccess ? e : done;
+}
+
 }  // namespace
 }  // namespace dc
 
@@ -275,7 +288,7 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
     cudaGetLastError();
     return prompt_cuda(e, "plan allocation");
   }
-  e = cudaMemcpy(block, host.data(), bytes, cudaMemcpyHostToDevice);
+  e = dc::upload_now(block, host.data(), bytes);
   if (e != cudaSuccess) {
     cudaFree(block);
     return prompt_cuda(e, "plan upload");

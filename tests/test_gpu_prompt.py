@@ -293,3 +293,30 @@ def test_maxima_that_rise_by_powers_of_two(step, dtype):
         k[:, 0, 0] = (sign * step * math.log(2) * (torch.arange(900, device="cuda") // 128)).to(dtype)
         out, lse = dc.PromptPlan([900], 1, 64, q_heads=4).attend(q, k, v, with_lse=True)
         compare(out, lse, q, k, v, [900], [900])
+
+
+def test_a_fresh_plan_on_another_stream():
+    """Plans made and used at once on a stream that does not wait for the default one, which is busy all the while: the
+    plan has arrived when the call returns, and its making does not wait for that work."""
+    import random
+    r, side, plans = random.Random(3), torch.cuda.Stream(), []
+    cases = [[r.randint(1, 200) for _ in range(r.choice([1, 5, 40, 300]))] for _ in range(24)]
+    k_lens = [[n + r.choice([0, 300, 3000 // len(ls)]) for n in ls] for ls in cases]
+    data = [inputs(a, b, 2, 2, 64, BF, seed=i) for i, (a, b) in enumerate(zip(cases, k_lens))]
+    plans.append(dc.PromptPlan([1], 2, 64, q_heads=4).attend(*inputs([1], [1], 2, 2, 64, BF)))  # (what a first call sets up)
+    torch.cuda.synchronize()
+    outs, busy = [], torch.cuda.Event()
+    torch.cuda._sleep(1 << 30)  # half a second or more
+    busy.record()
+    for i, (a, b) in enumerate(zip(cases, k_lens)):
+        plans.append(dc.PromptPlan(a, 2, 64, q_heads=4, k_lens=b))
+        if i % 2:
+            with torch.cuda.stream(side):
+                outs.append(plans[-1].attend(*data[i], with_lse=True))
+        else:
+            outs.append(plans[-1].attend(*data[i], with_lse=True, stream=side))
+    side.synchronize()
+    assert not busy.query(), "the default stream's work was waited for"
+    torch.cuda.synchronize()
+    for i, (out, lse) in enumerate(outs):
+        compare(out, lse, *data[i], cases[i], k_lens[i])
