@@ -407,11 +407,13 @@ typedef struct dc_prompt_plan dc_prompt_plan;
  * (k_len < q_len) gets output 0. causal 0: every query sees every key. head_dim 64 or
  * 128, q_heads = kv_heads times 1 to 128, lengths >= 0. Allocates on the current
  * device and waits for its own upload (not for other work): the plan may be used on any
- * stream at once. */
+ * stream at once. Plans may be made and freed while a stream captures; one must outlive
+ * the graphs that its calls were captured into. */
 dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int q_heads, int kv_heads,
                                 int head_dim, int causal, dc_prompt_plan** out);
 
-/* Frees the plan (its calls must have finished). NULL is a no-op. */
+/* Frees the plan (its calls must have finished, and the graphs that hold them be gone or
+ * never replay again). NULL is a no-op. */
 dc_status dc_prompt_plan_destroy(dc_prompt_plan* p);
 
 /* Tensors of dc_prompt_attend; strides in elements, the innermost one is 1. */

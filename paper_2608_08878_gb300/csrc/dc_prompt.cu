@@ -71,6 +71,19 @@ dc_status prompt_cuda(cudaError_t e, const char* what) {
 
 constexpr unsigned kPlanMagic = 0x44435050u;  // "DCPP"
 
+// While one lives, this thread's allocations, frees and waits are no part of a stream capture that is under way here or in
+// another thread: under the default mode each of them is refused, and the capture lost.
+class OutsideCapture {
+ public:
+  OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+  ~OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+  OutsideCapture(const OutsideCapture&) = delete;
+  OutsideCapture& operator=(const OutsideCapture&) = delete;
+
+ private:
+  cudaStreamCaptureMode mode_ = cudaStreamCaptureModeRelaxed;
+};
+
 // Copies to the device and waits until it is there, whatever stream the next call is on. (cudaMemcpy may return once
 // pageable memory is staged, and orders the rest on the legacy stream only, which a non-blocking stream does not wait
 // for; and it waits for all that the legacy stream is busy with. A stream of its own does neither.)
@@ -282,6 +295,7 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
   std::copy_n((const char*)v.first.data(), v.first.size() * sizeof(int), host.data() + at_first);
   std::copy_n((const char*)v.merges.data(), v.merges.size() * sizeof(int2), host.data() + at_merges);
   auto p = std::make_unique<dc_prompt_plan>();
+  const dc::OutsideCapture outside;
   char* block = nullptr;
   e = cudaMalloc(&block, bytes);
   if (e != cudaSuccess) {
@@ -318,7 +332,10 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
 dc_status dc_prompt_plan_destroy(dc_prompt_plan* p) {
   if (!p) return DC_OK;
   if (p->magic != dc::kPlanMagic) return DC_ERR_INVALID_ARG;
-  cudaFree(p->status);
+  {
+    const dc::OutsideCapture outside;
+    cudaFree(p->status);
+  }
   p->magic = 0;
   delete p;
   return DC_OK;

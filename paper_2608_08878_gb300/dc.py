@@ -463,7 +463,7 @@ def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps:
 class PromptPlan:
     """The division of the work of attention over packed sequences of given lengths (see
     dc_prompt_plan_create), on the current CUDA device; one plan serves every layer of a forward pass. It may be
-    used on any stream at once."""
+    used on any stream at once; keep it for as long as a CUDA graph that its calls were captured into."""
 
     def __init__(self, q_lens, kv_heads: int, head_dim: int, *, q_heads: int | None = None, k_lens=None,
                  causal: bool = True):

@@ -320,3 +320,24 @@ def test_a_fresh_plan_on_another_stream():
     torch.cuda.synchronize()
     for i, (out, lse) in enumerate(outs):
         compare(out, lse, *data[i], cases[i], k_lens[i])
+
+
+def test_plans_come_and_go_during_a_capture():
+    """A plan dropped while a stream captures (by the garbage collector, say), and one made and used there."""
+    lens = [70, 130]
+    q, k, v = inputs(lens, lens, 2, 4, 64, BF)
+    old = [dc.PromptPlan([n], 2, 64, q_heads=8) for n in (5, 300)]
+    want = dc.PromptPlan(lens, 2, 64, q_heads=8).attend(q, k, v)
+    out, graph = torch.zeros_like(want), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        old.pop()
+        plan = dc.PromptPlan(lens, 2, 64, q_heads=8)
+        plan.attend(q, k, v, out=out)
+        old[0].close()
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    plan.check()
