@@ -1,6 +1,7 @@
 // dc_prompt.cu -- attention of packed prompts (dc_prompt_plan_create,
 // dc_prompt_attend): the plan's work items and the C ABI.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <functional>
@@ -86,14 +87,21 @@ class OutsideCapture {
 
 // Copies to the device and waits until it is there, whatever stream the next call is on. (cudaMemcpy may return once
 // pageable memory is staged, and orders the rest on the legacy stream only, which a non-blocking stream does not wait
-// for; and it waits for all that the legacy stream is busy with. A stream of its own does neither.)
+// for; and it waits for all that the legacy stream is busy with. A stream of its own does neither. It is kept, one a
+// device: making one took 18 us of a small plan's 39.)
 cudaError_t upload_now(void* dst, const void* src, size_t bytes) {
-  cudaStream_t s = nullptr;
-  cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
-  if (e != cudaSuccess) return e;
-  e = cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, s);
-  const cudaError_t done = cudaStreamSynchronize(s);
-  cudaStreamDestroy(s);
+  static std::atomic<cudaStream_t> kept[kDevices];
+  const int dev = device_slot();
+  cudaStream_t s = dev >= 0 ? kept[dev].load(std::memory_order_acquire) : nullptr;
+  bool drop = false;
+  if (!s) {
+    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e != cudaSuccess) return e;
+    cudaStream_t none = nullptr;
+    drop = dev < 0 || !kept[dev].compare_exchange_strong(none, s);
+  }
+  const cudaError_t e = cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, s), done = cudaStreamSynchronize(s);
+  if (drop) cudaStreamDestroy(s);
   return e != cudaSuccess ? e : done;
 }
 
