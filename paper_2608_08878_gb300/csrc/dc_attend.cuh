@@ -46,9 +46,20 @@ struct AttnArgs {
   int two;  // whether items are two rows of one query tile each
   const int* rowlen;         // each row's length, or null (n)
   const int* parents;        // [batch][nodes]
+  unsigned long long wait_ns;  // att_wait_ns of the longest item
   unsigned* status;
   unsigned* dbg;
 };
+
+// How long a wait of the attention kernel may take before it gives up: the pipeline's own share, and what the other
+// roles stand still while attend_row goes over an item of this many keys (a warp's 32 rows, the keys twice each: 18 us
+// a key measured, 0.73 s for 40000; five times that).
+#ifdef DC_DEBUG_BOUNDS
+constexpr unsigned long long kAttWaitNs = 500000000ull;  // (so that a test can tell the two apart)
+#else
+constexpr unsigned long long kAttWaitNs = 10000000000ull;
+#endif
+inline unsigned long long att_wait_ns(long long keys) { return kAttWaitNs + 90000ull * (unsigned long long)keys; }
 
 // Two tiles of query rows (A, then B) of one KV head and the keys they see.
 struct AttnItem {

@@ -69,8 +69,6 @@ constexpr int kAttThreads = 384;
 constexpr int kAttRegsRow = 216, kAttRegsIssue = 72;
 constexpr int kAttCols = 512;
 constexpr int kItemRing = 4;  // items published ahead
-// Longer than mbar_wait's own limit: the other roles wait while attend_row goes over a long row.
-constexpr uint64_t kAttWaitNs = 10000000000ull;
 
 template <int D>
 struct AttSmem {
@@ -176,14 +174,14 @@ struct Steps {
 // counts: with mbar_wait's record at each of the twenty waits, one copy of each warp's loads and one
 // of the result's reads (129 -> 105 KB), trees of 8 nodes over 4096 rows of 410 tokens went from
 // 285 to 197 us, a prompt of 4096 from 93.5 to 91.2 us.
-__device__ __forceinline__ bool att_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site) {
+__device__ __forceinline__ bool att_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int site, uint64_t limit_ns) {
   if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
 #pragma unroll 1
   for (;;) {
     if (mbar_try_wait(bar, parity)) return true;
     if (*abort) return false;
-    if (globaltimer_ns() - t0 > kAttWaitNs) {
+    if (globaltimer_ns() - t0 > limit_ns) {
       *abort = site;
       return false;
     }
@@ -365,10 +363,11 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   grid_dep_launch();  // the partial results' merge, if any, may get ready
   const int tpt = kAttRows / a.G;
 
+  auto wait = [&](uint64_t* b, uint32_t parity, int site) { return att_wait(b, parity, abort, site, a.wait_ns); };
   // Waits for published item number k; false: no more, or the wait gave up.
   auto ready = [&](int k, int site) {
     const int e = k % kItemRing;
-    return att_wait(&b_item[e], (k / kItemRing) & 1, abort, site) && ring[e].it.y >= 0;
+    return wait(&b_item[e], (k / kItemRing) & 1, site) && ring[e].it.y >= 0;
   };
 
   if (warp >= 8) {
@@ -403,7 +402,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         for (int k = 0; !*abort; ++k) {
           const AttnItem it = next;
           const int e = k % kItemRing;
-          if (!att_wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, abort, 200)) break;
+          if (!wait(&b_free[e], ((k / kItemRing) & 1) ^ 1, 200)) break;
           int4* p = reinterpret_cast<int4*>(ring + e);
           p[0] = make_int4(it.y, it.h, it.lb, it.t0);
           p[1] = make_int4(it.tend, it.k0, it.klen, it.off);
@@ -416,7 +415,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           if (it.y < 0) break;
           fetch();
           if (st.n == 0) continue;
-          if (!att_wait(b_qempty, (sent & 1) ^ 1, abort, 201)) break;
+          if (!wait(b_qempty, (sent & 1) ^ 1, 201)) break;
           const bool two = TREE && st.alt == 2;
           mbar_expect_tx(b_qfull, st.alt == 1 ? qbytes : 2 * qbytes);
           for (int x = 0; x < (st.alt == 1 ? 1 : 2); ++x)
@@ -428,7 +427,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           for (int p2 = 0; p2 < 2 * st.n; ++p2) {
             bool v;
             const int i = st.load(p2, v), j = st.tile(i), s = g % ST;
-            if (!att_wait(&b_empty[s], ((g / ST) & 1) ^ 1, abort, 202)) break;
+            if (!wait(&b_empty[s], ((g / ST) & 1) ^ 1, 202)) break;
             mbar_expect_tx(&b_full[s], L::TILE);
             const bool d = TREE && j == st.draft;
             const CUtensorMap* tm = d ? (v ? &tmVD : &tmKD) : v ? &tmV : &tmK;
@@ -460,10 +459,10 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             mbar_arrive(&b_free[k % kItemRing]);
             continue;
           }
-          ok = att_wait(b_qfull, items, abort, 204);
+          ok = wait(b_qfull, items, 204);
           if (!ok) break;
           items ^= 1u;
-          auto full = [&](const Place<ST>& p) { return att_wait(&b_full[p.s], p.phase, abort, 205); };
+          auto full = [&](const Place<ST>& p) { return wait(&b_full[p.s], p.phase, 205); };
           auto s_mma = [&](int x, uint32_t qlo, uint32_t stage) {
             const uint32_t klo = k_lo + stage * (L::TILE >> 4);
 #pragma unroll
@@ -477,7 +476,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
             const uint32_t vlo = v_lo + stage * (L::TILE >> 4);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              if (!att_wait(&b_p[2 * x + h], np[x], abort, 206)) return false;
+              if (!wait(&b_p[2 * x + h], np[x], 206)) return false;
               tc_fence_after();
 #pragma unroll
               for (int ks = 4 * h; ks < 4 * h + 4; ++ks)
@@ -575,7 +574,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         bool ok = true;
 #pragma unroll 1
         for (int p2 = 0; p2 < 2 * st.n; ++p2) {
-          ok = __all_sync(0xffffffffu, att_wait(&b_full[g.s], g.phase, abort, 208));
+          ok = __all_sync(0xffffffffu, wait(&b_full[g.s], g.phase, 208));
           if (!ok) break;
           bool v;
           const int i = st.load(p2, v), mk = v ? st.masked(i) : 0;
@@ -644,7 +643,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       const int jstep = TREE ? alt + 1 : -1 - alt;
 #pragma unroll 1
       for (int i = 0; i < steps; ++i, j += jstep) {
-        att_wait(&b_s[X], ns, abort, 210 + X);
+        wait(&b_s[X], ns, 210 + X);
         ns ^= 1u;
         if (busy) {
           tc_fence_after();
@@ -744,7 +743,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
 
       // ---------------------------------------------------------- the item's result
       // (all that does not need O goes before the wait for it)
-      att_wait(&b_look[k % kItemRing], (k / kItemRing) & 1, abort, 214);
+      wait(&b_look[k % kItemRing], (k / kItemRing) & 1, 214);
       const int found = flags[2 * (k % kItemRing)] | flags[2 * (k % kItemRing) + 1];
       const bool bad = alt ? found != 0 : (found >> X & 1) != 0;
       // of two results over the same rows, each warpgroup joins half the dims
@@ -754,7 +753,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         xch[X * 128 + row] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(&b_x[0]);
-        att_wait(&b_x[0], nx, abort, 215);
+        wait(&b_x[0], nx, 215);
         const float2 y = xch[(X ^ 1) * 128 + row];
         const float mm = fmaxf(m, y.x);
         other = ring[k % kItemRing].of[X ^ 1].z;
@@ -799,11 +798,11 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         fy *= inv;
       }
       if (steps) {
-        att_wait(&b_o[X], no, abort, 212 + X);
+        wait(&b_o[X], no, 212 + X);
         no ^= 1u;
       }
       // (the other's products: it has passed its earlier results, as its part of the exchange says)
-      if (other) att_wait(&b_o[X ^ 1], oo, abort, 213);
+      if (other) wait(&b_o[X ^ 1], oo, 213);
       oo ^= ring[k % kItemRing].of[X ^ 1].z ? 1u : 0u;
       tc_fence_after();
       if (bad) {
@@ -896,7 +895,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       if (alt) {
         // the other warpgroup has read this one's O and statistics before they are written again
         if (lane == 0) mbar_arrive(&b_x[1]);
-        att_wait(&b_x[1], nx, abort, 216);
+        wait(&b_x[1], nx, 216);
         nx ^= 1u;
       }
       if (lane == 0) mbar_arrive(&b_free[k % kItemRing]);

@@ -114,6 +114,7 @@ struct dc_prompt_plan {
   int q_heads = 0, kv_heads = 0, head_dim = 0;
   long long q_tokens = 0, k_tokens = 0;
   int n_items = 0, n_merges = 0, n_slots = 0, prows = 0, grid = 0, num_sms = 0;
+  int item_tiles = 0;  // key tiles of the longest item
   // device: one allocation, the status words first
   unsigned* status = nullptr;     // [0] status, [8..15] the first failure
   dc::AttnItem* items = nullptr;
@@ -327,6 +328,7 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
   p->n_slots = v.slots;
   p->prows = v.prows;
   p->grid = (int)v.first.size() - 1;
+  for (const dc::AttnItem& it : v.items) p->item_tiles = std::max(p->item_tiles, it.j1 - it.j0);
   p->status = (unsigned*)block;
   p->items = (dc::AttnItem*)(block + at_items);
   p->first = (int*)(block + at_first);
@@ -399,6 +401,7 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   a.part_rows = (long long)p->n_slots * p->prows;
   a.out_len = p->q_tokens * a.o_t;
   a.part_ml = (float2*)((float*)x.workspace + (size_t)p->n_slots * p->prows * p->head_dim);
+  a.wait_ns = dc::att_wait_ns((long long)p->item_tiles * dc::kAttTok);
   a.status = p->status;
   a.dbg = p->status + 8;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);

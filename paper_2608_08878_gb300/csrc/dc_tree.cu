@@ -12,6 +12,7 @@ long long tree_plan(AttnArgs* a, int D, int num_sms) {
   a->prows = a->nodes <= tpt ? a->nodes * a->G : 256;
   a->n_items = a->rows * a->pairs;
   a->tiles = (a->n + kAttTok - 1) / kAttTok + 1;
+  a->wait_ns = att_wait_ns((long long)a->tiles * kAttTok);
   const long long total = (long long)a->n_items * a->tiles;  // (8 million at most in this GPU's memory)
   if (total >= 1ll << 30) return -1;
   // CTAs: every SM an equal share of a line's key tiles, but at least 2 tiles; or, of few items,

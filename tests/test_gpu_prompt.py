@@ -341,3 +341,22 @@ def test_plans_come_and_go_during_a_capture():
         torch.cuda.synchronize()
         assert torch.equal(out, want)
     plan.check()
+
+
+def test_rows_computed_anew_over_many_keys():
+    """A NaN among the last values: all rows of the items that must not see it are computed anew, which takes over a second
+    (the waits of a debug build would give up after half of one if they did not count the keys). Keys and values of the
+    heads overlap in memory."""
+    n, d, group, ql = 60000, 64, 4, 64
+    heads = torch.cuda.get_device_properties(0).multi_processor_count  # (an item each, none in parts)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn((ql, heads * group, d), device="cuda", generator=g).to(BF)
+    kb, vb = (torch.randn(8 * (n + heads) + d, device="cuda", generator=g).to(BF) for _ in range(2))
+    vb[8 * (n - 1):] = math.nan  # (of the first head's values, dims of the last eight)
+    k, v = (x.as_strided((n, heads, d), (8, 8, 1)) for x in (kb, vb))
+    plan = dc.PromptPlan([ql], heads, d, q_heads=heads * group, k_lens=[n])
+    assert plan.workspace_bytes == 0
+    out, lse = plan.attend(q, k, v, with_lse=True)
+    plan.check()
+    some = slice(0, 2 * group)
+    compare(out[:, some], lse[:, some], q[:, some], k[:, :2], v[:, :2], [ql], [n])
