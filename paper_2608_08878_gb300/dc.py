@@ -350,6 +350,26 @@ def _heads(t, name: str, heads: int | None, dim: int | None, dtype, device: int)
     return p, st, sh
 
 
+def _order(t, name: str, shape, *also) -> None:
+    """Checks that a tensor whose elements are counted already has them in this shape's order: a tensor of as many
+    dimensions must have the shape (or one of `also`), one of more or fewer must be a view of it (neighbouring
+    dimensions joined, or dimensions split)."""
+    got = t.shape
+    if got == shape or got in also or t.numel() == 0:
+        return
+
+    def ends(dims):  # the products of the last dimensions
+        n, out = 1, {1}
+        for x in reversed(dims):
+            n *= x
+            out.add(n)
+        return out
+
+    mine, theirs = ends(got), ends(shape)
+    if len(got) == len(shape) or not (mine <= theirs or theirs <= mine):
+        raise DCError(DC_ERR_INVALID_ARG, f"{name} has shape {tuple(got)}, expected {shape}")
+
+
 def _fresh(t, name: str, shape) -> None:
     """Checks that the output tensor t has this shape and no two places for one value."""
     if tuple(t.shape) != tuple(shape):
@@ -706,13 +726,22 @@ class DistillCache:
         pq = _arg(q, "q", torch.bfloat16, n * self.q_heads, device=self.device)
         pk = _arg(k_draft, "k_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         pv = _arg(v_draft, "v_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
-        if out is None:
+        of_q = (self.layers, self.batch, T, self.q_heads, self.head_dim)
+        grouped = (self.layers * self.batch, T, self.kv_heads, self.group, self.head_dim)
+        of_kv = (self.layers, self.batch, self.kv_heads, T, self.head_dim)
+        _order(q, "q", of_q, grouped)
+        _order(k_draft, "k_draft", of_kv)
+        _order(v_draft, "v_draft", of_kv)
+        given = out is not None
+        if not given:
             if _raw_stream(self.device) == self.stream.cuda_stream:
                 out = torch.empty_like(q, memory_format=torch.contiguous_format)
             else:  # (what the cache's stream writes belongs to that stream)
                 with torch.cuda.stream(self.stream):
                     out = torch.empty_like(q, memory_format=torch.contiguous_format)
         po = _arg(out, "out", torch.bfloat16, n * self.q_heads, device=self.device)
+        if given:
+            _order(out, "out", of_q, grouped)
         self._check(lib().dc_tree_attend(self._h, pq, pk, pv, pp, T, po))
         return out
 

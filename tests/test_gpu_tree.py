@@ -300,3 +300,21 @@ def test_queries_of_unused_nodes_may_hold_anything(rows, group, d, n, T, bad):
     cache.sync()
     assert bool((out[:, :, T // 2] == 0).all())
     assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+def test_drafts_and_queries_the_other_way_round_are_refused():
+    """[nodes][heads] where [heads][nodes] is meant, and the reverse, dense: as many elements, another order."""
+    cache, (q, kd, vd, parents) = make(1, 3, 2, 2, 64, 30, 4)
+    swap = lambda t: t.transpose(2, 3).contiguous()  # noqa: E731
+    want = cache.tree_attend(q, kd, vd, parents)
+    q5, k5, v5, p5 = rand(1, 3, 5, 4, 64), rand(1, 3, 2, 5, 64, seed=1), rand(1, 3, 2, 5, 64, seed=2), tree(3, 5, "chain")
+    bad = {"k_draft": (q, swap(kd), vd, parents), "v_draft": (q, kd, swap(vd), parents), "q": (swap(q5), k5, v5, p5),
+           "out": (q5, k5, v5, p5, torch.empty_like(swap(q5)))}
+    for what, args in bad.items():
+        with pytest.raises(dc.DCError) as e:
+            cache.tree_attend(*args)
+        assert e.value.status == dc.DC_ERR_INVALID_ARG and what in str(e.value)
+    # views in the same order are as good
+    for qv, kv in ((q[0], kd[0]), (q.view(3, 4, 2, 2, 64), kd.view(6, 4, 64)), (q.view(1, 3, 4, 256), kd.view(-1)),
+                   (q.view(1, 3, 4, 2, 2, 64), kd)):
+        assert torch.equal(cache.tree_attend(qv, kv, vd, parents).view(-1), want.view(-1))

@@ -124,3 +124,16 @@ def test_the_plain_attention_in_64_bits():
         check((p @ vz * 1.02).to(torch.bfloat16), o, tol)
     with pytest.raises(AssertionError):
         check(torch.full_like(o, float("nan")), o, tol)
+
+
+def test_the_order_of_a_tensors_dimensions():
+    """Drafts [layers][batch][kv_heads][nodes][d]: that shape and views of it; nodes and heads the other way round are refused."""
+    shape = (2, 3, 4, 8, 64)
+    for got in (shape, (6, 4, 8, 64), (24, 8, 64), (24, 512), (2 * 3 * 4 * 8 * 64,), (2, 3, 2, 2, 8, 64), (2, 3, 4, 8, 2, 32)):
+        dc._order(torch.empty(got, device="meta"), "k_draft", shape)
+    for got in ((2, 3, 8, 4, 64), (6, 8, 4, 64), (2, 3, 4, 64, 8), (3, 2, 4, 8, 64), (2, 3, 8, 2, 2, 64)):
+        with pytest.raises(dc.DCError) as e:
+            dc._order(torch.empty(got, device="meta"), "k_draft", shape)
+        assert e.value.status == dc.DC_ERR_INVALID_ARG, got
+    dc._order(torch.empty((6, 5, 2, 4, 64), device="meta"), "q", (2, 3, 5, 8, 64), (6, 5, 2, 4, 64))
+    dc._order(torch.empty((2, 3, 0, 8, 64), device="meta"), "q", (2, 3, 0, 8, 64))
