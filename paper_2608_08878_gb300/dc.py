@@ -480,6 +480,15 @@ def norm_rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, *, eps:
     return q_out, k_out
 
 
+def _lengths(x, name: str):
+    """The lengths as int32, after checking that they are whole numbers of that range."""
+    a = np.asarray(x)
+    if a.dtype != np.int32:
+        if a.dtype.kind not in "iuf" or not bool(((a >= -2.0 ** 31) & (a < 2.0 ** 31) & (np.floor(a) == a)).all()):
+            raise DCError(DC_ERR_INVALID_ARG, f"{name} must be whole numbers that fit int32")
+    return np.ascontiguousarray(a, dtype=np.int32).ravel()
+
+
 class PromptPlan:
     """The division of the work of attention over packed sequences of given lengths (see
     dc_prompt_plan_create), on the current CUDA device; one plan serves every layer of a forward pass. It may be
@@ -488,8 +497,8 @@ class PromptPlan:
     def __init__(self, q_lens, kv_heads: int, head_dim: int, *, q_heads: int | None = None, k_lens=None,
                  causal: bool = True):
         import torch
-        ql = np.ascontiguousarray(q_lens, dtype=np.int32).ravel()
-        kl = ql if k_lens is None else np.ascontiguousarray(k_lens, dtype=np.int32).ravel()
+        ql = _lengths(q_lens, "q_lens")
+        kl = ql if k_lens is None else _lengths(k_lens, "k_lens")
         if kl.size != ql.size:
             raise DCError(DC_ERR_INVALID_ARG, f"{ql.size} query lengths, {kl.size} key lengths")
         self._p = None

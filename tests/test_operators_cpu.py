@@ -137,3 +137,20 @@ def test_the_order_of_a_tensors_dimensions():
         assert e.value.status == dc.DC_ERR_INVALID_ARG, got
     dc._order(torch.empty((6, 5, 2, 4, 64), device="meta"), "q", (2, 3, 5, 8, 64), (6, 5, 2, 4, 64))
     dc._order(torch.empty((2, 3, 0, 8, 64), device="meta"), "q", (2, 3, 0, 8, 64))
+
+
+@pytest.mark.parametrize("bad", [np.asarray([2 ** 32 + 5]), [4, 2 ** 31], [-2 ** 31 - 1], [4.7], [float("nan")], [float("inf"), 3],
+                                 np.asarray([2 ** 63 + 8], dtype=np.uint64), ["4"], [None], [2 ** 70]])
+def test_lengths_that_int32_does_not_hold_are_refused(bad):
+    for call in (lambda: dc.PromptPlan(bad, 2, 64), lambda: dc.PromptPlan([3] * len(bad), 2, 64, k_lens=bad)):
+        with pytest.raises(dc.DCError) as e:
+            call()
+        assert e.value.status == dc.DC_ERR_INVALID_ARG
+
+
+def test_lengths_of_any_whole_type():
+    for x in ([5, 0, 300], np.asarray([5, 0, 300]), (5.0, 0.0, 300.0), np.asarray([5, 0, 300], dtype=np.uint16),
+              torch.tensor([5, 0, 300]), torch.tensor([5, 0, 300], dtype=torch.int32), np.asarray([[5, 0, 300]])):
+        got = dc._lengths(x, "q_lens")
+        assert got.dtype == np.int32 and got.flags.c_contiguous and got.tolist() == [5, 0, 300]
+    assert dc._lengths([], "q_lens").size == 0
