@@ -290,6 +290,11 @@ dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int
     kt += k_lens[s];
   }
   if (qt > (1 << 29) || kt > (1 << 29)) return prompt_fail(DC_ERR_INVALID_ARG, "at most 2^29 packed tokens");
+  // (64 bytes an item, and their numbers are ints)
+  long long count = 0;
+  const int item_tokens = 2 * (dc::kAttRows / (q_heads / kv_heads));
+  for (int s = 0; s < n; ++s) count += ((long long)q_lens[s] + item_tokens - 1) / item_tokens * kv_heads;
+  if (count > (1 << 29)) return prompt_fail(DC_ERR_INVALID_ARG, "too much work: at most 2^29 items of 256 query rows");
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);

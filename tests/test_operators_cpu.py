@@ -154,3 +154,12 @@ def test_lengths_of_any_whole_type():
         got = dc._lengths(x, "q_lens")
         assert got.dtype == np.int32 and got.flags.c_contiguous and got.tolist() == [5, 0, 300]
     assert dc._lengths([], "q_lens").size == 0
+
+
+@pytest.mark.parametrize("lens,hq,hk", [([1 << 29], 65535 * 128, 65535), ([1] * 20000, 65535, 65535), ([1 << 22] * 3, 65535 * 8, 65535)])
+def test_more_work_than_a_plan_counts_is_refused(lens, hq, hk):
+    """Items are numbered by ints and take 64 bytes each on the host and the device: refused before any is made."""
+    ql = np.asarray(lens, dtype=np.int32)
+    p = C.c_void_p()
+    st = dc.lib().dc_prompt_plan_create(ql.ctypes.data_as(C.c_void_p), None, ql.size, hq, hk, 64, 1, C.byref(p))
+    assert st == dc.DC_ERR_INVALID_ARG and not p.value and b"items" in dc.lib().dc_prompt_last_error()
