@@ -360,3 +360,24 @@ def test_rows_computed_anew_over_many_keys():
     plan.check()
     some = slice(0, 2 * group)
     compare(out[:, some], lse[:, some], q[:, some], k[:, :2], v[:, :2], [ql], [n])
+
+
+@pytest.mark.parametrize("dtype", [HF, BF])
+@pytest.mark.parametrize("n,bits", [(4096, -18.0), (131072, -21.6), (131072, -24.6), (131072, -25.0), (1 << 20, -24.6), (1 << 20, -25.2)])
+def test_many_small_weights_beside_a_large_one(n, bits, dtype):
+    """One key of weight 1 and a value of 0, n - 1 others of 2^bits each with values of 1, in items that are not divided.
+    In fp16 their weights are below the normal range: each is off by 2^-30 of the largest at most."""
+    rows, d = 256 * torch.cuda.get_device_properties(0).multi_processor_count, 64
+    q = torch.zeros((rows, 1, d), dtype=dtype, device="cuda")
+    k, v = torch.zeros((n, 1, d), dtype=dtype, device="cuda"), torch.ones((n, 1, d), dtype=dtype, device="cuda")
+    q[..., 0] = 1.0
+    k[: n - 1, 0, 0] = bits * math.log(2) / 0.125
+    v[n - 1] = 0.0
+    plan = dc.PromptPlan([rows], 1, d, q_heads=1, k_lens=[n], causal=False)
+    out = plan.attend(q, k, v)
+    plan.check()
+    w = (n - 1) * math.exp(0.125 * float(k[0, 0, 0]))
+    want = w / (1 + w)
+    u = torch.finfo(dtype).eps / 2
+    tol = 1.02 * 2 * u * want + (n * 2.0 ** -30 + 2.0 ** -25 if dtype == HF else 0)
+    assert float((out.double() - want).abs().max()) <= tol
