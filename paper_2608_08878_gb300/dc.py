@@ -741,9 +741,9 @@ class DistillCache:
         _order(q, "q", of_q, grouped)
         _order(k_draft, "k_draft", of_kv)
         _order(v_draft, "v_draft", of_kv)
-        given = out is not None
+        given, elsewhere = out is not None, _raw_stream(self.device) != self.stream.cuda_stream
         if not given:
-            if _raw_stream(self.device) == self.stream.cuda_stream:
+            if not elsewhere:
                 out = torch.empty_like(q, memory_format=torch.contiguous_format)
             else:  # (what the cache's stream writes belongs to that stream)
                 with torch.cuda.stream(self.stream):
@@ -751,6 +751,9 @@ class DistillCache:
         po = _arg(out, "out", torch.bfloat16, n * self.q_heads, device=self.device)
         if given:
             _order(out, "out", of_q, grouped)
+        if elsewhere:  # (their memory may not go to other tensors before that stream has read them)
+            for t in (q, k_draft, v_draft, parents, out):
+                t.record_stream(self.stream)
         self._check(lib().dc_tree_attend(self._h, pq, pk, pv, pp, T, po))
         return out
 

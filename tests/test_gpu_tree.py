@@ -318,3 +318,29 @@ def test_drafts_and_queries_the_other_way_round_are_refused():
     for qv, kv in ((q[0], kd[0]), (q.view(3, 4, 2, 2, 64), kd.view(6, 4, 64)), (q.view(1, 3, 4, 256), kd.view(-1)),
                    (q.view(1, 3, 4, 2, 2, 64), kd)):
         assert torch.equal(cache.tree_attend(qv, kv, vd, parents).view(-1), want.view(-1))
+
+
+def test_inputs_of_another_stream_are_kept_until_they_are_read():
+    """The cache on a stream of its own that is busy; the caller drops the inputs, and the default stream's next tensors
+    would take their places."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        cache, kept = make(1, 2, 2, 4, 64, 300, 6)
+    for busy in (False, True):  # (first launches load kernels, and wait)
+        torch.cuda.synchronize()
+        draft = [t.clone() for t in kept]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            if busy:
+                torch.cuda._sleep(1 << 28)
+            done = torch.cuda.Event()
+        out = cache.tree_attend(*draft)
+        done.record(side)
+        shapes = [(t.shape, t.dtype) for t in draft]
+        draft.clear()
+        over = [torch.full(s, 1, dtype=d, device="cuda") for s, d in shapes]
+        torch.cuda.current_stream().synchronize()
+        assert not busy or not done.query()
+        torch.cuda.synchronize()
+        compare(cache, kept, out)
+        del over
