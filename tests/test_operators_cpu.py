@@ -163,3 +163,30 @@ def test_more_work_than_a_plan_counts_is_refused(lens, hq, hk):
     p = C.c_void_p()
     st = dc.lib().dc_prompt_plan_create(ql.ctypes.data_as(C.c_void_p), None, ql.size, hq, hk, 64, 1, C.byref(p))
     assert st == dc.DC_ERR_INVALID_ARG and not p.value and b"items" in dc.lib().dc_prompt_last_error()
+
+
+@pytest.mark.parametrize("n,d,dtype", [(20000, 128, torch.bfloat16), (30000, 128, torch.bfloat16), (50001, 64, torch.bfloat16),
+                                       (70001, 64, torch.bfloat16), (33333, 128, torch.float16)])
+def test_marked_values_show_a_tile_that_is_lost_or_read_twice(n, d, dtype):
+    """The comparison of long rows with values of marked() does not let one whole key tile of 128 by, wherever it is."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+    from attention64 import attention64, check
+    from marks import marked
+    g = torch.Generator().manual_seed(n)
+    q, k = (torch.randn(s, generator=g).to(dtype) for s in ((2, d), (n, d)))
+    v = marked(n, d, dtype, "cpu", 5)
+    seen = torch.ones((2, n), dtype=torch.bool)
+    o, _, tol, _ = attention64(q, k, v, seen, d ** -0.5)
+    check(o.to(dtype), o, tol)
+    tiles = n // 128
+    for t in {0, 1, tiles // 2, tiles - 1} | set(torch.randint(0, tiles, (4,), generator=g).tolist()):
+        at = slice(t * 128, t * 128 + 128)
+        seen[:, at] = False
+        less = attention64(q, k, v, seen, d ** -0.5)[0]
+        seen[:, at] = True
+        twice = attention64(q, torch.cat([k, k[at]]), torch.cat([v, v[at]]), torch.ones((2, n + 128), dtype=torch.bool), d ** -0.5)[0]
+        for wrong in (less, twice):
+            with pytest.raises(AssertionError):
+                check(wrong.to(dtype), o, tol)
