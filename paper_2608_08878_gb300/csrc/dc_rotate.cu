@@ -52,14 +52,14 @@ struct Bf16 {
   }
 };
 
-// f / 2 pi as a 64-bit fraction of a turn: f times 1 / 2 pi in two 24-bit parts,
+// f / 2 pi as a 64-bit fraction of a turn, of either sign: f times 1 / 2 pi in two 24-bit parts,
 // the products' rounding errors kept.
 __device__ __forceinline__ unsigned long long turn_fraction(float f) {
   constexpr float hi = 0x1.45f306p-3f, lo = 0x1.b9391p-28f;  // 1 / (2 pi) = hi + lo + 2^-54
   const float p = __fmul_rn(f, hi);
   const float e = __fmaf_rn(f, lo, __fmaf_rn(f, hi, -p));
-  const float r = p - floorf(p);  // exact: whole turns do not matter, the position is whole
-  return 2ull * ((unsigned long long)(r * 0x1p63f) + (unsigned long long)(long long)(e * 0x1p63f));
+  const float r = p - truncf(p);  // exact (p - floor(p) is not, below 0): whole turns do not matter, the position is whole
+  return 2ull * (unsigned long long)((long long)(r * 0x1p63f) + (long long)(e * 0x1p63f));
 }
 
 // Two 32-bit values in one 64-bit register, for the paired arithmetic of sm_100.

@@ -204,3 +204,19 @@ def test_refusals():
         with pytest.raises(dc.DCError) as e:
             call()
         assert e.value.status == dc.DC_ERR_INVALID_ARG, what
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_frequencies_of_either_sign(interleaved):
+    """Negative frequencies turn the other way, as exactly: against 64 bits, as negative positions do, and back again."""
+    q, k, pos, f, _ = inputs(600, 4, 2, 128, 128, HF)
+    pos = pos * 16  # to 2^21
+    f = f * torch.where(torch.arange(64, device="cuda") % 3 == 0, -1.0, 1.0)
+    f[1], f[2], f[4] = -7.5, -1e-8, -1.0
+    for x in (f, -f, -f.abs()):
+        qo, ko = dc.norm_rotate(q, k, pos, x, norm=False, interleaved=interleaved)
+        check(qo, want64(q, pos, x, None, False, interleaved))
+        check(ko, want64(k, pos, x, None, False, interleaved))
+        assert torch.equal(dc.norm_rotate(q, k, -pos, -x, norm=False, interleaved=interleaved)[0], qo)
+        back = dc.norm_rotate(qo, ko, pos, -x, norm=False, interleaved=interleaved)[0]
+        assert float((back.float() - q.float()).abs().max()) <= 4 * U[HF] * float(q.abs().max())
