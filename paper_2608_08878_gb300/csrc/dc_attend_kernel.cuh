@@ -624,7 +624,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + X * 128, t_o = tmem + lanes + 256 + X * 128;
     uint4* const buf = reinterpret_cast<uint4*>(smem + L::OUT + warp * 4096);
-    const float c = a.c, grow = Mma<T>::kAbove / c, room = Mma<T>::kRoom / c;
+    const float c = a.c, grow = Mma<T>::kAbove / c;
+    // (finite, so that a scale near the smallest there is leaves m finite)
+    const float room = Mma<T>::kRoom > 0.f ? fminf(Mma<T>::kRoom / c, 1e38f) : 0.f;
     const int row_t = row / a.G, row_g = row % a.G;
     uint32_t ns = 0, no = 0, oo = 0, nx = 0;  // S tiles, results (oo: the other's) and exchanges so far, modulo 2
     for (int k = 0; __all_sync(0xffffffffu, ready(k, 209)); ++k) {

@@ -381,3 +381,11 @@ def test_many_small_weights_beside_a_large_one(n, bits, dtype):
     u = torch.finfo(dtype).eps / 2
     tol = 1.02 * 2 * u * want + (n * 2.0 ** -30 + 2.0 ** -25 if dtype == HF else 0)
     assert float((out.double() - want).abs().max()) <= tol
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("scale", [1e-30, 1.2e-38, 1e-38, 1e-39, 1e-42])
+def test_the_smallest_scales(scale, dtype):
+    q, k, v = inputs([300], [300], 1, 4, 64, dtype)
+    out, lse = dc.PromptPlan([300], 1, 64, q_heads=4).attend(q, k, v, with_lse=True, scale=scale)
+    compare(out, lse, q, k, v, [300], [300], scale=scale)
