@@ -88,3 +88,36 @@ def test_random_rows():
         out = cache.tree_attend(*draft)
         cache.sync()
         compare(cache, draft, out)
+
+
+@pytest.mark.parametrize("kw", [dict(global_tokens=True), dict(scorer=1), dict(scorer=2), dict(alpha_mode=1), dict(engine=1),
+                                dict(budget_ratio=0.3)])
+def test_caches_of_every_kind(kw):
+    cache, draft = make(2, 2, 2, 4, 128, 700, 20, **kw)
+    for i in range(3):
+        cache.step(rand(2, 2, 8, 128, seed=8 + i), rand(2, 2, 2, 128, seed=19 + i), rand(2, 2, 2, 128, seed=30 + i), budget=300 - 50 * i)
+        compare(cache, draft, cache.tree_attend(*draft))
+    cache.sync()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(engine=1), dict(global_tokens=True), dict(scorer=1)])
+def test_steps_are_the_same_with_trees_between(kw):
+    """Before a step and between a step's scores and its eviction, with rows in parts: all results and the cache bit for bit."""
+    runs = []
+    for between in (False, True):
+        cache, draft = make(2, 2, 4, 4, 128, 3000, 12, **kw)
+        got = []
+        for i in range(6):
+            x = (rand(2, 2, 16, 128, seed=8 + i), rand(2, 2, 4, 128, seed=90 + i), rand(2, 2, 4, 128, seed=50 + i))
+            if between:
+                cache.tree_attend(*draft)
+            if i % 2:
+                got.append(cache.step(*x, budget=2000 - i))
+                continue
+            got.append(cache.decode_step(*x))
+            if between:
+                cache.tree_attend(*draft)
+            cache.evict(2000 - i)
+        cache.sync()
+        runs.append(got + [cache.buffer(b)[:, :1995] for b in (dc.BUF_K, dc.BUF_V, dc.BUF_POS)])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
