@@ -51,13 +51,15 @@ struct AttnArgs {
   unsigned* dbg;
 };
 
-// How long a wait of the attention kernel may take before it gives up: the pipeline's own share, and what the other
-// roles stand still while attend_row goes over an item of this many keys (a warp's 32 rows, the keys twice each: 18 us
-// a key measured, 0.73 s for 40000; five times that).
+// How long a wait of the attention kernel may take before it gives up: kAttWaitNs, and where an item has more than
+// kAttLongKeys keys what the other roles stand still while attend_row goes over it (a warp's 32 rows, the keys twice each:
+// 18 us a key measured, 0.73 s for 40000; five times that).
 #ifdef DC_DEBUG_BOUNDS
 constexpr unsigned long long kAttWaitNs = 500000000ull;  // (so that a test can tell the two apart)
+constexpr long long kAttLongKeys = 8192;
 #else
 constexpr unsigned long long kAttWaitNs = 10000000000ull;
+constexpr long long kAttLongKeys = 262144;
 #endif
 inline unsigned long long att_wait_ns(long long keys) { return kAttWaitNs + 90000ull * (unsigned long long)keys; }
 

@@ -299,7 +299,9 @@ __device__ __forceinline__ void flush_rows(const uint4* buf, uint8_t* const (&to
     if (on >> (i * 4 + lane / 8) & 1u) *reinterpret_cast<uint4*>(to[i] + at) = v[i];
 }
 
-template <class T, int D, bool TREE>
+// LONG: some item has more keys than kAttLongKeys, and the waits take AttnArgs::wait_ns (which as an operand of every
+// wait costs 1 to 2% of any prompt: 5340 us instead of 5250 for 32768 tokens).
+template <class T, int D, bool TREE, bool LONG>
 __global__ void __launch_bounds__(kAttThreads, 1)
     attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKD,
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   grid_dep_launch();  // the partial results' merge, if any, may get ready
   const int tpt = kAttRows / a.G;
 
-  auto wait = [&](uint64_t* b, uint32_t parity, int site) { return att_wait(b, parity, abort, site, a.wait_ns); };
+  auto wait = [&](uint64_t* b, uint32_t parity, int site) { return att_wait(b, parity, abort, site, LONG ? a.wait_ns : kAttWaitNs); };
   // Waits for published item number k; false: no more, or the wait gave up.
   auto ready = [&](int k, int site) {
     const int e = k % kItemRing;
@@ -843,7 +845,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       } else if (busy) {
         const int d0 = alt ? X * (D / 2) : 0, d1 = alt ? d0 + D / 2 : D;
         // (an unused node's O holds what its query made of the cached tokens: NaN, of a query that is)
-        const bool blank = __any_sync(0xffffffffu, !sees);
+        const bool blank = TREE && __any_sync(0xffffffffu, !sees);
         // 32 dims of this row's result
         auto dims = [&](int d, float (&o)[32]) {
           if (steps) {
@@ -1030,13 +1032,20 @@ struct AttMaps {
   CUtensorMap q, k, v, kd, vd;
 };
 
+template <class T, int D, bool TREE, bool LONG>
+cudaError_t launch_attend_kernel(const AttMaps& m, const AttnArgs& a, int grid, cudaStream_t s) {
+  static SmemLimit limit;
+  if (cudaError_t e = limit.raise(attend_kernel<T, D, TREE, LONG>, AttSmem<D>::BYTES); e != cudaSuccess) return e;
+  // (its set-up may run under the end of the kernel before it)
+  return launch_pdl(attend_kernel<T, D, TREE, LONG>, dim3(grid), dim3(kAttThreads), AttSmem<D>::BYTES, s, m.q, m.k, m.v, m.kd,
+                    m.vd, a);
+}
+
 template <class T, int D, bool TREE>
 cudaError_t launch_attend(const AttMaps& m, const AttnArgs& a, int grid, cudaStream_t s) {
-  static SmemLimit limit;
-  if (cudaError_t e = limit.raise(attend_kernel<T, D, TREE>, AttSmem<D>::BYTES); e != cudaSuccess) return e;
-  // (its set-up may run under the end of the kernel before it)
-  if (cudaError_t e = launch_pdl(attend_kernel<T, D, TREE>, dim3(grid), dim3(kAttThreads), AttSmem<D>::BYTES, s, m.q, m.k, m.v,
-                                 m.kd, m.vd, a);
+  const bool is_long = a.wait_ns > att_wait_ns(kAttLongKeys);
+  if (cudaError_t e = is_long ? launch_attend_kernel<T, D, TREE, true>(m, a, grid, s)
+                              : launch_attend_kernel<T, D, TREE, false>(m, a, grid, s);
       e != cudaSuccess)
     return e;
   if (a.n_merges == 0) return cudaSuccess;

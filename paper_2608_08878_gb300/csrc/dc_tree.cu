@@ -12,7 +12,6 @@ long long tree_plan(AttnArgs* a, int D, int num_sms) {
   a->prows = a->nodes <= tpt ? a->nodes * a->G : 256;
   a->n_items = a->rows * a->pairs;
   a->tiles = (a->n + kAttTok - 1) / kAttTok + 1;
-  a->wait_ns = att_wait_ns((long long)a->tiles * kAttTok);
   const long long total = (long long)a->n_items * a->tiles;  // (8 million at most in this GPU's memory)
   if (total >= 1ll << 30) return -1;
   // CTAs: every SM an equal share of a line's key tiles, but at least 2 tiles; or, of few items,
@@ -26,6 +25,7 @@ long long tree_plan(AttnArgs* a, int D, int num_sms) {
   // 193 -> 133, 4096 x 1000 248 -> 208. Long rows read at the same rate either way, and parts of equal size
   // balance better than whole rows.
   a->two = a->rows > num_sms && a->nodes <= tpt && !a->rowlen && a->tiles * D <= 640;
+  int longest = a->tiles;  // key tiles of an item
   if (a->two) {
     a->tiles = 1;  // (a place is an item)
     a->line = (a->rows + 1) / 2;
@@ -33,6 +33,8 @@ long long tree_plan(AttnArgs* a, int D, int num_sms) {
   }
   a->per = a->line / a->ctas;
   a->extra = a->line % a->ctas;
+  if (!a->two) longest = std::min(longest, a->per + (a->extra ? 1 : 0));
+  a->wait_ns = att_wait_ns((long long)longest * kAttTok);
   const int grid = a->grid = a->ctas * a->pairs;
   bool cut = false;
   for (int b = 1; b < grid && !cut; ++b) cut = tree_from(*a, b) % a->tiles != 0;
