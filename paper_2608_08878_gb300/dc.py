@@ -736,11 +736,14 @@ class DistillCache:
         pk = _arg(k_draft, "k_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         pv = _arg(v_draft, "v_draft", torch.bfloat16, n * self.kv_heads, device=self.device)
         of_q = (self.layers, self.batch, T, self.q_heads, self.head_dim)
-        grouped = (self.layers * self.batch, T, self.kv_heads, self.group, self.head_dim)
         of_kv = (self.layers, self.batch, self.kv_heads, T, self.head_dim)
-        _order(q, "q", of_q, grouped)
-        _order(k_draft, "k_draft", of_kv)
-        _order(v_draft, "v_draft", of_kv)
+        grouped = (self.layers * self.batch, T, self.kv_heads, self.group, self.head_dim)
+        if q.shape != of_q:
+            _order(q, "q", of_q, grouped)
+        if k_draft.shape != of_kv:
+            _order(k_draft, "k_draft", of_kv)
+        if v_draft.shape != of_kv:
+            _order(v_draft, "v_draft", of_kv)
         given, elsewhere = out is not None, _raw_stream(self.device) != self.stream.cuda_stream
         if not given:
             if not elsewhere:
