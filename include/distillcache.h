@@ -385,8 +385,8 @@ typedef struct {
 /* Norms of queries and keys for each head and the position rotation in one pass:
  * y = x / sqrt(mean(x^2) + eps) * w (or y = x), pairs (a, b) of y's first rotary_dim dims
  * become (a cos t - b sin t, b cos t + a sin t) with t = position * inv_freq[j]. In 32
- * bits, rounded once; the angle is reduced exactly, so that large positions lose
- * nothing. Every head must start on 16 bytes (strides multiples of 8). Outputs must not
+ * bits, rounded once; the angle is off by at most 1e-7 + 5e-15 |position * inv_freq| rad,
+ * for frequencies of either sign below 2^26. Every head must start on 16 bytes (strides multiples of 8). Outputs must not
  * overlap inputs other than by being them. DC_ERR_INVALID_ARG (message in
  * dc_rotate_last_error()) for anything else. */
 dc_status dc_norm_rotate(const dc_rotate_args* args, void* stream);
@@ -412,7 +412,7 @@ typedef struct dc_prompt_plan dc_prompt_plan;
 dc_status dc_prompt_plan_create(const int* q_lens, const int* k_lens, int n, int q_heads, int kv_heads,
                                 int head_dim, int causal, dc_prompt_plan** out);
 
-/* Frees the plan (its calls must have finished, and the graphs that hold them be gone or
+/* Frees the plan, which may wait for the device (its calls must have finished, and the graphs that hold them be gone or
  * never replay again). NULL is a no-op. */
 dc_status dc_prompt_plan_destroy(dc_prompt_plan* p);
 
@@ -435,7 +435,8 @@ dc_status dc_prompt_workspace(const dc_prompt_plan* p, size_t* bytes);
 
 /* Softmax attention as planned; query head j uses KV head j / (q_heads / kv_heads).
  * Sums and statistics in 32 bits, the weights rounded to `dtype` for the second
- * product, one rounding of the output. A key or value that a query does not see
+ * product (in fp16 n small ones are off by n 2^-30 of the largest at most), one rounding
+ * of the output, which must not overlap q, k or v. A key or value that a query does not see
  * leaves its output alone, whatever it holds; lse is -infinity where a query sees
  * no key. 16-byte aligned tensors, strides multiples of 8. */
 dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, void* stream);

@@ -16,9 +16,10 @@
 // take more (99; 5 blocks an SM, all resident, 114).
 //
 // Angles: the fraction of a turn that pos * f_j leaves is pos * (f_j / 2 pi) modulo
-// 1. f_j / 2 pi is held as a 64-bit fraction (48 good bits), whose product with the
-// integer position wraps exactly; the top 32 bits go to sincospif. The error stays below
-// 1e-6 rad up to position 2^21, where an angle in 32-bit floating point is off by 0.06.
+// 1. f_j / 2 pi is held as a 64-bit fraction (about 50 good bits), whose product with the
+// integer position wraps exactly; the top 32 bits go to sincospif. The angle is off by at most
+// 1e-7 + 5e-15 |pos * f_j| rad (5e-7 at position 2^21 and f_j 100; an angle of 2^21 in 32-bit floating
+// point is off by 0.06), for f_j of either sign below 2^26.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
