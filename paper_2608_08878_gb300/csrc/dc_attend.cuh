@@ -162,9 +162,9 @@ __device__ __noinline__ void attend_row(const AttnArgs& a, const uint16_t* q, co
     for (int j = 0; j < a.nodes; ++j)
       if (w[j >> 5] >> (j & 31) & 1u) best(kd + (long long)j * D);
   {
-    const float mc = m == -INFINITY ? 0.f : m * a.c;
+    const float ref = m == -INFINITY ? 0.f : m;
     auto key = [&](const uint16_t* kj, const uint16_t* vj) {
-      const float p = exp2f(fmaf(dot(kj), a.c, -mc));
+      const float p = exp2f((dot(kj) - ref) * a.c);
       l += p;
 #pragma unroll
       for (int e = 0; e < E; ++e) {

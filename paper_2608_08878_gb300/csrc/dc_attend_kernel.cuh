@@ -74,6 +74,7 @@ constexpr int kAttThreads = 384;
 constexpr int kAttRegsRow = 216, kAttRegsIssue = 72;
 constexpr int kAttCols = 512;
 constexpr int kItemRing = 4;  // items published ahead
+constexpr float kAttFar = 1024.f;  // a reference (in log2) beyond which it is taken from the scores before they are scaled
 
 template <int D>
 struct AttSmem {
@@ -684,6 +685,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
       if (drafts && valid) sees = tree_mask(a.parents + (long long)(lb % a.batch) * a.nodes, t, nodes);
 
       float m = -INFINITY, l = 0.f;
+      bool far = false;  // whether some row's reference is
       int j = TREE ? it.j0 + of.y : it.j1 - 1 - of.y;
       const int jstep = TREE ? alt + 1 : -1 - alt;
 #pragma unroll 1
@@ -731,15 +733,17 @@ __global__ void __launch_bounds__(kAttThreads, 1)
           };
           float mx = fmaxf(top(0), top(1));
           if (live) mx = max3(mx, top(2), top(3));
-          const bool up = mx > m + grow;
+          const bool up = mx - m > grow;
           if (i == 0) {
             m = mx - room;
+            far = __any_sync(0xffffffffu, fabsf(m) * c > kAttFar && m != -INFINITY);
           } else if (__any_sync(0xffffffffu, up)) {
             const float f = up ? ex2((m - (mx - room)) * c) : 1.f;
             if (up) {
               m = mx - room;
               l *= f;
             }
+            far = __any_sync(0xffffffffu, fabsf(m) * c > kAttFar && m != -INFINITY);
 #pragma unroll 1
             for (int q = 0; q < D / 32; ++q) {
               float o[32];
@@ -751,7 +755,24 @@ __global__ void __launch_bounds__(kAttThreads, 1)
               tmem_st32(t_o + q * 32, r);
             }
           }
-          const float mc = m == -INFINITY ? 0.f : m * c;
+          float mc = m == -INFINITY ? 0.f : m * c;
+          // s c - m c with m c rounded: all weights of this reference have 2^(the rounding) as a factor. It cancels, but not
+          // against other references', nor where it leaves the type: so far from 0 the difference goes first. (For all rows:
+          // 4096 tokens, 64 heads of 64 dims 154.4 us instead of 151.2; without either 149.9. The rows of a warp that are not
+          // far keep their bits.)
+          if (__builtin_expect(far, 0)) {
+            const float from = fabsf(mc) > kAttFar ? m : 0.f;
+            if (from != 0.f) mc = 0.f;
+            const uint64_t from2 = pair2(-from, -from);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                const float2 x = unpair2(add2(pair2(s[q][e], s[q][e + 1]), from2));
+                s[q][e] = x.x;
+                s[q][e + 1] = x.y;
+              }
+          }
           const uint64_t c2 = pair2(c, c), mc2 = pair2(-mc, -mc);
           uint64_t sum[2] = {0, 0};  // pairs of 0.f
 #pragma unroll

@@ -51,10 +51,10 @@ struct PagedAttn {
   uint16_t* out;
   float* lse;
   float* part;      // [2 grid][rows][D], with shared prefixes then [S kvh blocks][rows][D]: sums of weighted values
-  float2* part_ml;  // likewise: the weights' reference (in log2) and their sum
+  float2* part_ml;  // likewise: the weights' reference, a score, and their sum
   int* line;        // each sequence's first place, all places, the CTAs that took them
   float* pre;       // [places][prows][D]: of the prefixes
-  float2* pre_ml;   // likewise, the reference as a score
+  float2* pre_ml;   // likewise
   int rows, grid;
   int blocks;       // units of a sequence and KV head: its query heads in blocks of `rows`
   int whole;        // whether no unit is cut

@@ -26,7 +26,8 @@
 //
 // P is rounded to the cache's type because both operands of a product have one type: half a unit in the last place
 // of each weight, of the order of the result's own rounding; l sums the weights unrounded. In
-// fp16 the weights are up to 2^14 instead of 1, so that those above 2^-28 of the largest keep all their bits.
+// fp16 the weights are up to 2^14 instead of 1, so that those above 2^-28 of the largest keep all their bits (taken back
+// where the warps' results are joined).
 #include <algorithm>
 
 #include "dc_device.h"
@@ -446,10 +447,11 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
           uint32_t p[NT][2];
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const float m0 = m[t][0] == -INFINITY ? 0.f : fmaf(m[t][0], -c2, Frag<T>::kRoom);
-            const float m1 = m[t][1] == -INFINITY ? 0.f : fmaf(m[t][1], -c2, Frag<T>::kRoom);
-            const float p0 = ex2(fmaf(z[t][0], c2, m0)), p1 = ex2(fmaf(z[t][1], c2, m1));
-            const float p2 = ex2(fmaf(z[t][2], c2, m0)), p3 = ex2(fmaf(z[t][3], c2, m1));
+            // (the difference first: the rounding of m c alone is a factor of any size where scores are far from 0)
+            constexpr float up2 = Frag<T>::kRoom;
+            const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
+            const float p0 = ex2(fmaf(z[t][0] - m0, c2, up2)), p1 = ex2(fmaf(z[t][1] - m1, c2, up2));
+            const float p2 = ex2(fmaf(z[t][2] - m0, c2, up2)), p3 = ex2(fmaf(z[t][3] - m1, c2, up2));
             l[t][0] += p0 + p2;
             l[t][1] += p1 + p3;
             p[t][0] = transpose8(T::pack(p0, p1));
@@ -477,7 +479,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
           x += __shfl_xor_sync(0xffffffffu, x, 8);
           x += __shfl_xor_sync(0xffffffffu, x, 16);
           const int r = t * 8 + lane % 4 * 2 + e;
-          if (lane < 4) red_ml[warp * RB + r] = make_float2(m[t][e] == -INFINITY ? -INFINITY : fmaf(m[t][e], c2, -Frag<T>::kRoom), x);
+          if (lane < 4) red_ml[warp * RB + r] = make_float2(m[t][e], x);
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) {
             float* to_d = red + (warp * RB + r) * L::RED_ROW + d * 16 + lane / 4;
@@ -505,7 +507,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
         for (int w = 0; w < WARPS; ++w) {
           // (scores of NaN alone leave a reference of -infinity and a sum of NaN)
           if (ml[w].x == -INFINITY && ml[w].y == 0.f) continue;
-          const float f = ml[w].x == -INFINITY ? 1.f : ex2(ml[w].x - mm);
+          const float f = ml[w].x == -INFINITY ? 1.f : ex2(fmaf(ml[w].x - mm, c2, -Frag<T>::kRoom));
           sum = fmaf(f, ml[w].y, sum);
           const float* from_w = red + (w * RB + r) * L::RED_ROW + lane * E;
 #pragma unroll
@@ -528,7 +530,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
           uint32_t* to_o = reinterpret_cast<uint32_t*>(a.out + row * D) + lane * (E / 2);
           if constexpr (E == 4) *reinterpret_cast<uint2*>(to_o) = make_uint2(y[0], y[1]);
           else *to_o = y[0];
-          if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(mm, 0.6931471805599453f, logf(sum));
+          if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(mm, a.scale, logf(sum));
         }
       }
       consumers_sync<32 * WARPS>();
@@ -573,7 +575,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
   if (!joined && n1 == 1) return;  // (the result is there already)
   const int first = (n1 == 1 ? 2 * a.grid + s * units + unit : 2 * b0 + 1) * RB + rr, second = (2 * b0 + 2) * RB + rr;
   float mm = -INFINITY, sum = 0.f, x[E] = {};
-  // (the prefix's statistics hold the reference as a score, and a sum of -1 where a row saw nothing)
+  // (a reference is a score; the prefix's statistics hold a sum of -1 where a row saw nothing)
   auto load = [&](int i) {
     if (i < n1) {
       const int p = i == 0 ? first : second + (i - 1) * 2 * RB;
@@ -582,7 +584,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
     const long long p = pre + (long long)(i - n1) * a.sh.prows;
     if (i >= n1 + n2 || !DC_INB(a.c, p, (long long)a.sh.places * a.sh.prows, 412)) return make_float2(-INFINITY, 0.f);
     const float2 v = a.pre_ml[p];
-    return v.y < 0.f ? make_float2(-INFINITY, 0.f) : make_float2(v.x == -INFINITY ? v.x : v.x * a.c2, v.y);
+    return v.y < 0.f ? make_float2(-INFINITY, 0.f) : v;
   };
   auto sums = [&](int i) {
     const float* p = i < n1 ? a.part + (long long)(i == 0 ? first : second + (i - 1) * 2 * RB) * D
@@ -598,7 +600,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
   for (int i0 = 0; i0 < parts; i0 += 32) {
     const float2 v = i0 ? load(i0 + lane) : v0;
     // (scores of NaN alone leave a reference of -infinity and a sum of NaN)
-    const float f = v.x == -INFINITY ? (v.y != v.y ? 1.f : 0.f) : ex2(v.x - mm);
+    const float f = v.x == -INFINITY ? (v.y != v.y ? 1.f : 0.f) : ex2((v.x - mm) * a.c2);
     if (i0 + lane < parts) sum = fmaf(f, v.y, sum);
     const int n = min(32, parts - i0);
 #pragma unroll
@@ -639,7 +641,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
   uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (long long)row * D) + lane * (E / 2);
   if constexpr (E == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
   else *to = y[0];
-  if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(mm, 0.6931471805599453f, logf(sum));
+  if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(mm, a.scale, logf(sum));
 }
 
 template <class T, int D, int NT>
