@@ -375,7 +375,9 @@ __global__ void __launch_bounds__(kAttThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   grid_dep_wait();    // all inputs, and the outputs' and partial results' last readers
-  grid_dep_launch();  // the partial results' merge, if any, may get ready
+  // The partial results' merge, if any, may get ready. Over pages paged_attend_kernel starts here, and reads what this
+  // kernel has waited for without a wait of its own: for it the wait must stay before this, in every thread that gets here.
+  grid_dep_launch();
   const int tpt = kAttRows / a.G;
 
   auto wait = [&](uint64_t* b, uint32_t parity, int site) { return att_wait(b, parity, abort, site, LONG ? a.wait_ns : kAttWaitNs); };

@@ -108,10 +108,14 @@ constexpr int kPagSeqs = 4096;  // sequences of a call, at most
 struct SeqRun {
   int from, n, len;
 };
+// BEHIND: from L2, as said where the kernel begins.
+template <bool BEHIND>
+__device__ __forceinline__ int from_table(const int* p) { return BEHIND ? __ldcg(p) : __ldg(p); }
+template <bool BEHIND>
 __device__ __forceinline__ SeqRun seq_run(const PagedAttn& a, int s) {
   SeqRun r;
   const long long room = (long long)a.W << a.c.log;
-  r.len = (int)min((long long)max(0, __ldg(a.lens + s)), room);
+  r.len = (int)min((long long)max(0, from_table<BEHIND>(a.lens + s)), room);
   r.from = s < a.sh.seqs ? __ldg(a.sh.prefix + s) : 0;
   r.n = r.len < r.from ? 0 : r.len - r.from;
   if (r.len < r.from) r.len = 0;
@@ -134,7 +138,8 @@ struct PagCut {
   }
 };
 
-template <class T, int D, int NT>
+// BEHIND: launched behind the prefixes' kernel.
+template <class T, int D, int NT, bool BEHIND>
 __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
     paged_attend_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                         const __grid_constant__ PagedAttn a) {
@@ -165,10 +170,11 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
     fence_mbar_init();
   }
   if (warp >= WARPS && lane == 0) prefetch_tmap(warp > WARPS ? &tmV : &tmK);
-  // (Behind the prefixes' kernel, which has waited for all before it and is not needed until its results are
-  // joined, this one starts beside it and waits for it at the end.)
-  const bool behind = a.sh.grid > 0;
-  if (!behind) grid_dep_wait();
+  // (Behind the prefixes' kernel, which is not needed until its results are joined, this one starts beside it and waits for it
+  // at the end. What came before that kernel is complete: each of its blocks waits before it lets this one start. This one's
+  // own wait, which would also say so to its L1 caches, comes too late: lengths and page numbers are read from L2, where
+  // TMA reads the rest.)
+  if (!BEHIND) grid_dep_wait();
   grid_dep_launch();
   if (warp >= WARPS && lane == 0) fence_proxy_async_global();  // (the producer's: what threads of earlier kernels wrote)
 
@@ -178,8 +184,8 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
   {
     auto places = [&](int s) {
       if (s >= a.S) return 0;
-      if (blockIdx.x == 0 && __ldg(a.lens + s) > ((long long)a.W << a.c.log)) atomicOr(a.c.status, kStatusBadPage);
-      return units * (START + max(1, (int)(((unsigned)run_tokens(a, seq_run(a, s)) + kPagTok - 1) / kPagTok)));
+      if (blockIdx.x == 0 && from_table<BEHIND>(a.lens + s) > ((long long)a.W << a.c.log)) atomicOr(a.c.status, kStatusBadPage);
+      return units * (START + max(1, (int)(((unsigned)run_tokens(a, seq_run<BEHIND>(a, s)) + kPagTok - 1) / kPagTok)));
     };
     int base = 0;
     for (int s0 = 0; s0 < a.S; s0 += THREADS) {
@@ -210,7 +216,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
     if (threadIdx.x == 0) a.line[a.S + 1] = ctas;
   }
   if ((int)blockIdx.x >= ctas) {
-    if (behind) grid_dep_wait();
+    if (BEHIND) grid_dep_wait();
     return;
   }
   const PagCut cut(total, ctas);
@@ -255,7 +261,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
         t = off - unit * len - START;
         h = a.blocks == 1 ? unit : unit % kvh;
         if (t >= 0) {
-          const SeqRun run = seq_run(a, s);
+          const SeqRun run = seq_run<BEHIND>(a, s);
           const int* sel = a.selected ? a.selected + (long long)(s * kvh + h) * a.count : nullptr;
           int x = (t << log_n) + (lane & (nb - 1));  // the box's place in the selection, then in the sequence
           bool there = true;
@@ -271,7 +277,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
           }
           const long long tok = (long long)x << log_b;
           if (there && tok < run.len) {
-            const int page = __ldg(a.tables + (long long)s * a.W + (x >> log_p));
+            const int page = from_table<BEHIND>(a.tables + (long long)s * a.W + (x >> log_p));
             if (page < 0 || page >= a.c.pages) {
               atomicOr(a.c.status, kStatusBadPage);
             } else {
@@ -538,12 +544,13 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
   }
   __syncthreads();
   if (threadIdx.x == 0 && *abort) atomicOr(a.c.status, kStatusTimeout);
-  if (behind) grid_dep_wait();
+  if (BEHIND) grid_dep_wait();
 }
 
 // Joins the parts of one query row, a block each: those of its sequence's own tokens, then those of the prefix that it
 // shares. Lane i of every warp takes the statistics of part i, 32 at a time; the parts' sums are shared out to the
 // four warps, whose loads are all in flight at once, and added up in a fixed order.
+// (Before its wait only what the host uploaded may be read.)
 constexpr int kMergeWarps = 4;
 template <class T, int D>
 __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __grid_constant__ PagedAttn a) {
@@ -554,9 +561,8 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
   const int RB = a.rows, units = a.blocks * a.c.kvh, block = a.blocks == 1 ? 0 : r / RB, unit = block * a.c.kvh + h, rr = r - block * RB;
   // parts of the prefix: n2 of them, prows rows apart
   const bool joined = s < a.sh.seqs;
-  int n2 = 0;
+  int n2 = 0, least = 0;
   long long pre = 0;
-  bool blind = false;
   if (joined) {
     const int g = __ldg(a.sh.group + s), tokens = __ldg(a.sh.prefix + s), tpt = kAttRows / a.c.G;
     const int i = s - __ldg(a.sh.first + g), pair = i / (2 * tpt), in = i - pair * 2 * tpt;
@@ -565,9 +571,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
       n2 = run.y;
       pre = (long long)run.x * a.sh.prows + (in >= tpt ? kAttRows : 0) + (in >= tpt ? in - tpt : in) * a.c.G + r;
     }
-    blind = __ldg(a.lens + s) < max(1, tokens);
+    least = max(1, tokens);
   }
   grid_dep_wait();
+  const int len = joined ? a.lens[s] : 0;  // (looked at at the end: before the parts' loads it takes 2.7 us of 64 sequences' merge)
   // parts of its own tokens: n1; the first one's row, the second one's, the others 2 RB apart
   const int total = a.line[a.S], ctas = a.line[a.S + 1], at = a.line[s], ul = (a.line[s + 1] - at) / units, x0 = at + unit * ul;
   const PagCut cut(total, ctas);
@@ -591,7 +598,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
                             : a.pre + (pre + (long long)(i - n1) * a.sh.prows) * D;
     return p + lane * E;
   };
-  const int parts = blind ? 0 : n1 + n2;
+  const int parts = n1 + n2;
   const float2 v0 = load(lane);  // (32 parts or fewer: read once)
   mm = v0.x;
   for (int i = 32; i < parts; i += 32) mm = fmaxf(mm, load(i + lane).x);
@@ -634,6 +641,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
     for (int e = 0; e < E; ++e) x[e] += shared[w][lane * E + e];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (joined && len < least) sum = 0.f;  // a sequence that is shorter than its prefix, or not in use, sees nothing
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   uint32_t y[E / 2];
 #pragma unroll
@@ -644,24 +652,28 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
   if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(mm, a.scale, logf(sum));
 }
 
-template <class T, int D, int NT>
+template <class T, int D, int NT, bool BEHIND>
 cudaError_t launch(const PagedAttn& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
   static SmemLimit limit;
-  if (cudaError_t e = limit.raise(paged_attend_kernel<T, D, NT>, PagSmem<D, NT>::LINE + (kPagSeqs + 1) * 4); e != cudaSuccess)
+  if (cudaError_t e = limit.raise(paged_attend_kernel<T, D, NT, BEHIND>, PagSmem<D, NT>::LINE + (kPagSeqs + 1) * 4); e != cudaSuccess)
     return e;
   const size_t bytes = PagSmem<D, NT>::LINE + (size_t)(a.S + 1) * 4;
-  if (cudaError_t e = launch_pdl(paged_attend_kernel<T, D, NT>, dim3(a.grid), dim3(PagSmem<D, NT>::THREADS), bytes, s, k, v, a); e != cudaSuccess)
+  if (cudaError_t e = launch_pdl(paged_attend_kernel<T, D, NT, BEHIND>, dim3(a.grid), dim3(PagSmem<D, NT>::THREADS), bytes, s, k, v, a); e != cudaSuccess)
     return e;
   if (a.whole) return cudaSuccess;
   const int rows = a.S * a.c.qh;  // (4096 * 1024 * 128 at most)
   return launch_pdl(paged_merge_kernel<T, D>, dim3((unsigned)rows), dim3(32 * kMergeWarps), 0, s, a);
 }
 
-template <class T, int D>
+template <class T, int D, bool BEHIND>
 cudaError_t launch_rows(const PagedAttn& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
-  if (a.rows == 8) return launch<T, D, 1>(a, k, v, s);
-  if (a.rows == 16) return launch<T, D, 2>(a, k, v, s);
-  return launch<T, D, 4>(a, k, v, s);
+  if (a.rows == 8) return launch<T, D, 1, BEHIND>(a, k, v, s);
+  if (a.rows == 16) return launch<T, D, 2, BEHIND>(a, k, v, s);
+  return launch<T, D, 4, BEHIND>(a, k, v, s);
+}
+template <class T, int D>
+cudaError_t launch_any(const PagedAttn& a, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
+  return a.sh.grid > 0 ? launch_rows<T, D, true>(a, k, v, s) : launch_rows<T, D, false>(a, k, v, s);
 }
 
 static_assert(PagSmem<128, 1>::LINE + (kPagSeqs + 1) * 4 <= 232448 && PagSmem<128, 2>::LINE + (kPagSeqs + 1) * 4 <= 232448 &&
@@ -708,8 +720,8 @@ size_t paged_workspace(PagedAttn* a, int D, int num_sms, char* base) {
 }
 
 cudaError_t launch_paged_attend(const PagedAttn& a, int D, int dtype, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
-  if (dtype == DC_BF16) return D == 128 ? launch_rows<Bf16, 128>(a, k, v, s) : launch_rows<Bf16, 64>(a, k, v, s);
-  return D == 128 ? launch_rows<Half, 128>(a, k, v, s) : launch_rows<Half, 64>(a, k, v, s);
+  if (dtype == DC_BF16) return D == 128 ? launch_any<Bf16, 128>(a, k, v, s) : launch_any<Bf16, 64>(a, k, v, s);
+  return D == 128 ? launch_any<Half, 128>(a, k, v, s) : launch_any<Half, 64>(a, k, v, s);
 }
 
 }  // namespace dc
