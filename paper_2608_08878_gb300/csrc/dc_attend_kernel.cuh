@@ -859,6 +859,7 @@ __global__ void __launch_bounds__(kAttThreads, 1)
         to[i] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(ro.out),
                                                        i * 4 + lane / 8)) + (lane & 7) * 16;
       const uint32_t on = __ballot_sync(0xffffffffu, writes);
+      // (PAGED: every row sees the whole prefix, and what is masked behind it came as zeros, which weights of 0 leave alone)
       if ((PAGED || !bad) && writes && (!alt || X == 0)) ro.stats(a, m, l);
       {
         const float inv = slot >= 0 ? 1.f : sees ? rcp(l) : 0.f;
