@@ -47,11 +47,15 @@ class ToyModel:
 
 
 def run(samples=4, tokens=40, pages=0, prompt_len=200, page=32, seed=0):
-    """[samples][tokens] sampled tokens; pages: of each sample and KV head in a step (0: all)."""
+    """([samples][tokens] sampled tokens, the prompt, the logits that the last of them was sampled from, the model); pages: of
+    each sample and KV head in a step (0: all)."""
+    if samples < 1 or tokens < 1 or prompt_len < 1 or pages < 0:
+        raise ValueError("needs samples, tokens and a prompt, and pages >= 0")
     g = torch.Generator(device="cuda").manual_seed(seed)
     model = ToyModel(seed=seed)
     prompt = torch.randint(0, model.vocab, (prompt_len,), device="cuda", generator=g)
-    shared = prompt_len // page * page  # whole pages; what is left of the prompt every sample stores for itself
+    # whole pages; what is left of the prompt, one token at least, every sample stores for itself
+    shared = (prompt_len - 1) // page * page
     width = -(-(prompt_len + tokens) // page)
     own = width - shared // page
     cache = dc.PagedCache(len(model.layers), shared // page + samples * own, model.kvh, model.d, page_size=page, q_heads=model.hq)
@@ -61,10 +65,11 @@ def run(samples=4, tokens=40, pages=0, prompt_len=200, page=32, seed=0):
 
     # the shared part of the prompt once, then each sample's rest of it
     head, rest = prompt[:shared], prompt[shared:]
-    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
-    keys = torch.empty((shared, model.kvh, model.d), dtype=BF, device="cuda")
-    plan = dc.PromptPlan([shared], model.kvh, model.d, q_heads=model.hq)
-    model.forward(head, cache, tables[:1].contiguous(), zero, lambda i, q, k, v: plan.attend(q, k, v), k_out=keys)
+    if shared:
+        zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+        keys = torch.empty((shared, model.kvh, model.d), dtype=BF, device="cuda")
+        plan = dc.PromptPlan([shared], model.kvh, model.d, q_heads=model.hq)
+        model.forward(head, cache, tables[:1].contiguous(), zero, lambda i, q, k, v: plan.attend(q, k, v), k_out=keys)
     prefixes = cache.share([samples], [shared])
     lens = torch.full((samples,), shared, dtype=torch.int32, device="cuda")
 
@@ -72,9 +77,10 @@ def run(samples=4, tokens=40, pages=0, prompt_len=200, page=32, seed=0):
         return cache.attend(q, tables, lens + 1, layer=i, shared=prefixes)
 
     def sparse(i, q, k, v):
-        return cache.attend(q, tables, lens + 1, layer=i, selected=cache.select(q, tables, lens + 1, pages, layer=i, keep_last=2))
+        # the newest page always, then the first one, then the one before the newest, as far as there is room
+        selected = cache.select(q, tables, lens + 1, pages, layer=i, keep_first=min(1, pages - 1), keep_last=min(2, max(1, pages - 1)))
+        return cache.attend(q, tables, lens + 1, layer=i, selected=selected)
 
-    logits = None
     for t in rest.tolist():
         logits = model.forward(torch.full((samples,), t, device="cuda"), cache, tables, lens, dense)
         lens += 1
@@ -91,6 +97,9 @@ def run(samples=4, tokens=40, pages=0, prompt_len=200, page=32, seed=0):
     draw = lambda: -torch.log(-torch.log(torch.rand(noise.shape, device="cuda", generator=g).clamp(1e-9, 1 - 1e-7)))  # noqa: E731
     token.copy_((logits.float() + draw()).argmax(-1))
     out = [token.clone()]
+    if tokens == 1:
+        cache.check()
+        return torch.stack(out, 1), prompt, logits, model
     graph = torch.cuda.CUDAGraph()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -117,6 +126,8 @@ def main():
     p.add_argument("--tokens", type=int, default=40)
     p.add_argument("--pages", type=int, default=0, help="pages of each sample and KV head in a step (0: all)")
     a = p.parse_args()
+    if a.samples < 1 or a.tokens < 1 or a.pages < 0:
+        p.error("--samples and --tokens must be at least 1, --pages at least 0")
     out = run(a.samples, a.tokens, a.pages)[0]
     for i, row in enumerate(out.tolist()):
         print(f"sample {i}: {row}")
