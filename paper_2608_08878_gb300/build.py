@@ -11,7 +11,6 @@ Each translation unit compiles in parallel; nothing is installed elsewhere.
 from __future__ import annotations
 
 import concurrent.futures as cf
-import importlib.util
 import os
 import shutil
 import subprocess
@@ -93,19 +92,31 @@ def _link(objs: list[str], target: str, libs: list[str]) -> None:
 
 def _bind() -> str:
     src = os.path.join(CSRC, "dc_bind.cpp")
-    if _stale(LIB_BIND, [src, os.path.join(INCLUDE, "distillcache.h")]):
-        torch = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
-        cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    try:
+        import torch as installed
+    except ImportError as e:
+        raise RuntimeError(f"dc_bind.cpp is built against PyTorch's headers, and PyTorch cannot be imported: {e}") from e
+    torch = installed.__path__[0]
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    cmd = [os.environ.get("CXX") or shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", src,
+           f'-DDC_TORCH_VERSION="{installed.__version__}"', "-I", INCLUDE, "-isystem", os.path.join(torch, "include"),
+           "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(cuda, "include"), "-I", sysconfig.get_paths()["include"],
+           "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
+    # what the module was built against and how: other objects' layouts do not show in the sources' times
+    stamp, made_for = LIB_BIND + ".stamp", " ".join([sysconfig.get_config_var("SOABI") or sys.version] + cmd)
+    known = ""
+    if os.path.exists(stamp):
+        with open(stamp) as f:
+            known = f.read()
+    if known != made_for or _stale(LIB_BIND, [src, os.path.join(INCLUDE, "distillcache.h")]):
         tmp = LIB_BIND + f".tmp{os.getpid()}"
-        cmd = [os.environ.get("CXX") or shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", tmp,
-               "-I", INCLUDE, "-isystem", os.path.join(torch, "include"),
-               "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
-               "-isystem", os.path.join(cuda, "include"), "-I", sysconfig.get_paths()["include"],
-               "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
-        res = subprocess.run(cmd, capture_output=True, text=True)
+        res = subprocess.run(cmd + ["-o", tmp], capture_output=True, text=True)
         if res.returncode != 0:
             raise RuntimeError(f"{cmd[0]} failed for dc_bind.cpp:\n{res.stdout}\n{res.stderr}")
         os.replace(tmp, LIB_BIND)
+        with open(stamp, "w") as f:
+            f.write(made_for)
     return LIB_BIND
 
 

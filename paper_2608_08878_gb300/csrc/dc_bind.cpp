@@ -332,4 +332,11 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dc_bind", nullptr, -1, g_method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__dc_bind() { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__dc_bind() {
+  PyObject* m = PyModule_Create(&g_module);
+  // what it was built against
+  if (m && (PyModule_AddStringConstant(m, "torch", DC_TORCH_VERSION) < 0 ||
+            PyModule_AddObject(m, "python", PyUnicode_FromFormat("%d.%d", PY_MAJOR_VERSION, PY_MINOR_VERSION)) < 0))
+    Py_CLEAR(m);
+  return m;
+}

@@ -224,13 +224,22 @@ def _bind():
             if _bound is None:
                 import importlib.machinery
                 import importlib.util
-                import torch  # noqa: F401  (whose libraries it is linked against)
+                import sys
+                import torch  # (whose libraries it is linked against)
                 path = os.path.join(_HERE, "_dc_bind.so")
+                how = "build it with `python -m paper_2608_08878_gb300.build`"
                 if not os.path.exists(path):
-                    raise OSError(f"{path} is missing: build it with `python -m paper_2608_08878_gb300.build`")
+                    raise OSError(f"{path} is missing: {how}")
                 loader = importlib.machinery.ExtensionFileLoader("_dc_bind", path)
-                m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_dc_bind", loader))
-                loader.exec_module(m)
+                try:
+                    m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_dc_bind", loader))
+                    loader.exec_module(m)
+                except ImportError as e:
+                    raise OSError(f"{path} cannot be loaded ({e}): {how} anew") from e
+                # (it reads PyTorch's objects by the layout of the version that it was built against)
+                is_for, here = (m.torch, m.python), (str(torch.__version__), "%d.%d" % sys.version_info[:2])
+                if is_for != here:
+                    raise OSError(f"{path} is built for PyTorch {is_for[0]} and Python {is_for[1]}, not {here[0]} and {here[1]}: {how} anew")
                 m.library(*(C.cast(f, C.c_void_p).value for f in (L.dc_paged_append, L.dc_paged_attend,
                                                                    L.dc_paged_attend_workspace, L.dc_paged_select)))
                 _bound = m
