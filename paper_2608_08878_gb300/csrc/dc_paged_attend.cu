@@ -212,7 +212,8 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
   const int total = line[a.S];
   const int ctas = min((int)gridDim.x, max(1, a.whole ? total / (START + 1) : (total + kPagMinTiles - 1) / kPagMinTiles));
   if (blockIdx.x == 0 && !a.whole) {
-    for (int s = threadIdx.x; s <= a.S; s += THREADS) a.line[s] = line[s];
+    for (int s = threadIdx.x; s <= a.S; s += THREADS)
+      if (DC_INB(a.c, s, a.S + 2, 414)) a.line[s] = line[s];
     if (threadIdx.x == 0) a.line[a.S + 1] = ctas;
   }
   if ((int)blockIdx.x >= ctas) {
@@ -283,6 +284,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
             } else {
               n = (int)min((long long)PB, run.len - tok);
               y = ((page * kvh + h) << a.c.log) + (x & in_page) * PB;
+              if (!DC_INB(a.c, y + PB - 1, (long long)a.c.pages * kvh * a.c.page, 415)) n = 0;
             }
           }
         }
@@ -529,6 +531,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
           }
         } else {
           const long long row = (long long)s * a.c.qh + h * a.c.G + r0 + r;
+          if (!DC_INB(a.c, row, (long long)a.S * a.c.qh, 413)) continue;
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
           uint32_t y[E / 2];
 #pragma unroll
@@ -646,6 +649,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) paged_merge_kernel(const __g
   uint32_t y[E / 2];
 #pragma unroll
   for (int e = 0; e < E; e += 2) y[e / 2] = sum == 0.f ? 0u : T::pack(x[e] * inv, x[e + 1] * inv);
+  if (!DC_INB(a.c, row, (long long)a.S * a.c.qh, 416)) return;
   uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (long long)row * D) + lane * (E / 2);
   if constexpr (E == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
   else *to = y[0];

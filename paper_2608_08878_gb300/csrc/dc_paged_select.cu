@@ -127,8 +127,9 @@ __device__ __forceinline__ void score_pages(const SelectView& a, int s, int h, i
     uint32_t bad = 0u;
 #pragma unroll
     for (int i = 0; i < kSelRounds; ++i) {
-      const bool fine = (unsigned)page[i] < (unsigned)a.c.pages;
+      bool fine = (unsigned)page[i] < (unsigned)a.c.pages;
       if (!fine) bad |= 1u << i;
+      fine = fine && DC_INB(a.c, ((long long)page[i] * a.c.kvh + h) * 2 * LP + LP + l, (long long)a.c.pages * a.c.kvh * 2 * LP, 420);
       // (below 2^32: a layer has fewer than 2^27 heads of pages)
       const uint4* b = reinterpret_cast<const uint4*>(a.c.bounds) + (unsigned)((fine ? page[i] : 0) * a.c.kvh + h) * (unsigned)(2 * LP);
       hi[i] = __ldg(b + l);
@@ -263,10 +264,12 @@ __global__ void __launch_bounds__(kSelThreads, 1) page_select_kernel(const Selec
   grid_dep_launch();
   const int pages = a.pages_of(s);
   int* out = a.out + row * a.count;
+  const int* end = a.out + (long long)a.S * a.c.kvh * a.count;  // (debug builds: what every write is checked against)
   if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   if (pages <= a.count) {  // (the whole cluster)
     if (rank == 0)
-      for (int i = tid; i < a.count; i += kSelThreads) out[i] = i < pages ? i : -1;
+      for (int i = tid; i < a.count; i += kSelThreads)
+        if (DC_INB(a.c, out + i - a.out, end - a.out, 423)) out[i] = i < pages ? i : -1;
     return;
   }
   // n pages between those that are kept in any case, `need` of them
@@ -276,8 +279,10 @@ __global__ void __launch_bounds__(kSelThreads, 1) page_select_kernel(const Selec
   if (need > 0) {
     const int j0 = a.first + (int)((long long)n * rank / ctas), j1 = a.first + (int)((long long)n * (rank + 1) / ctas);
     score_pages<T, D>(a, s, h, j0, j1, [&](int j, uint32_t key) {
-      if (!all_near) far[j - a.first] = key;
-      else if (rank == 0) near[j - a.first] = key;
+      if (!DC_INB(a.c, j - a.first, min(n, all_near ? kSelKeys : a.W), 421)) return;
+      if (!all_near) {
+        if (DC_INB(a.c, row * a.W + j - a.first, (long long)a.S * a.c.kvh * a.W, 422)) far[j - a.first] = key;
+      } else if (rank == 0) near[j - a.first] = key;
       else sm100::st_cluster(sm100::cluster_addr(near + (j - a.first), 0), key);
     });
   }
@@ -287,8 +292,10 @@ __global__ void __launch_bounds__(kSelThreads, 1) page_select_kernel(const Selec
   } else {
     __syncthreads();
   }
-  for (int i = tid; i < a.first + a.last; i += kSelThreads)
-    out[i < a.first ? i : i + need] = i < a.first ? i : i + n;
+  for (int i = tid; i < a.first + a.last; i += kSelThreads) {
+    int* to = out + (i < a.first ? i : i + need);
+    if (DC_INB(a.c, to - a.out, end - a.out, 424)) *to = i < a.first ? i : i + n;
+  }
   if (need == 0) return;
   auto key = [&](int i) { return all_near ? near[i] : far[i]; };
   uint32_t least;
@@ -315,7 +322,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) page_select_kernel(const Selec
     const bool f = kept(i);
     const unsigned mk = __ballot_sync(0xffffffffu, f);
     const int to = at + __popc(mk & ((1u << lane) - 1u));
-    if (f && to < need) out[to] = a.first + i;
+    if (f && to < need && DC_INB(a.c, out + to - a.out, end - a.out, 425)) out[to] = a.first + i;
     at += __popc(mk);
   }
 }
