@@ -442,7 +442,8 @@ dc_status dc_prompt_workspace(const dc_prompt_plan* p, size_t* bytes);
 dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, void* stream);
 
 /* Waits for the stream; DC_ERR_DEVICE if a kernel of the plan has reported an error
- * (a wait inside it that ran out of time). */
+ * (a wait inside it that ran out of time). Captures that are under way are not disturbed; a stream that
+ * captures is refused. */
 dc_status dc_prompt_check(const dc_prompt_plan* p, void* stream);
 
 /* Message of the last failed dc_prompt_* call on this host thread. */
@@ -476,7 +477,8 @@ dc_status dc_paged_create(const dc_paged_config* cfg, dc_paged** out);
 dc_status dc_paged_destroy(dc_paged* h);
 
 /* Waits for the stream; DC_ERR_DEVICE if a kernel of this handle has reported an error since it was made: a page
- * number outside the pool, a position behind a table's end, starts out of order, a wait that ran out of time. */
+ * number outside the pool, a position behind a table's end, starts out of order, a wait that ran out of time. Captures that are under way are
+ * not disturbed; a stream that captures is refused. */
 dc_status dc_paged_check(dc_paged* h, void* stream);
 
 /* What dc_paged_append reads and writes; strides in elements, the innermost one is 1, every head starts on 16

@@ -139,9 +139,10 @@ dc_status dc_paged_destroy(dc_paged* h) {
 
 dc_status dc_paged_check(dc_paged* h, void* stream) {
   if (!h || h->magic != dc::kPagedMagic) return paged_fail(DC_ERR_INVALID_ARG, "not a paged cache");
-  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   unsigned st[16] = {};
-  if (e == cudaSuccess) e = cudaMemcpy(st, h->status, sizeof st, cudaMemcpyDeviceToHost);
+  bool captures = false;
+  const cudaError_t e = dc::fetch_status(static_cast<cudaStream_t>(stream), h->status, st, &captures);
+  if (captures) return paged_fail(DC_ERR_INVALID_ARG, "the stream is capturing: its calls have not run yet");
   if (e != cudaSuccess) return paged_cuda(e, "check");
   if (st[0]) {
     char buf[256];

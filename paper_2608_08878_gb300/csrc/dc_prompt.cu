@@ -406,9 +406,10 @@ dc_status dc_prompt_workspace(const dc_prompt_plan* p, size_t* bytes) {
 
 dc_status dc_prompt_check(const dc_prompt_plan* p, void* stream) {
   if (!p || p->magic != dc::kPlanMagic) return prompt_fail(DC_ERR_INVALID_ARG, "not a plan");
-  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   unsigned st[16] = {};
-  if (e == cudaSuccess) e = cudaMemcpy(st, p->status, sizeof st, cudaMemcpyDeviceToHost);
+  bool captures = false;
+  const cudaError_t e = dc::fetch_status(static_cast<cudaStream_t>(stream), p->status, st, &captures);
+  if (captures) return prompt_fail(DC_ERR_INVALID_ARG, "the stream is capturing: its calls have not run yet");
   if (e != cudaSuccess) return prompt_cuda(e, "check");
   if (st[0]) {
     char buf[160];
