@@ -362,7 +362,7 @@ dc_status dc_prompt_attend(const dc_prompt_plan* p, const dc_prompt_args* args, 
   a.G = p->q_heads / p->kv_heads;
   a.kvh = p->kv_heads;
   a.scale = x.scale;
-  a.c = (float)(1.4426950408889634 * x.scale);
+  a.c = (float)std::min(1.4426950408889634 * x.scale, 3.4e38);  // (finite for every scale)
   a.items = p->items;
   a.first = p->first;
   a.merges = p->merges;

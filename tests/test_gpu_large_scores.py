@@ -156,6 +156,24 @@ def test_prompts(base, step, scale, dtype, d):
         q0, k0 = q0 + ql, k0 + kl
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (HF, 64)])
+@pytest.mark.parametrize("scale", [1e38, 3e38])
+def test_prompts_at_the_largest_scales(scale, dtype, d):
+    """scale times log2(e) is past what 32 bits hold: the keys of the largest score share the weight."""
+    g = torch.Generator(device="cuda").manual_seed(10)
+    n, kvh, group = 300, 2, 4
+    q = torch.randint(-1, 2, (n, kvh * group, d), device="cuda", generator=g).to(dtype)
+    k = torch.randint(-1, 2, (n, kvh, d), device="cuda", generator=g).to(dtype)
+    v = torch.randn((n, kvh, d), device="cuda", generator=g).to(dtype)
+    plan = dc.PromptPlan([n], kvh, d, q_heads=kvh * group)
+    out = plan.attend(q, k, v, scale=scale)
+    plan.check()
+    x = q.view(n, kvh, group, d).permute(1, 2, 0, 3)
+    seen = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+    o, _, tol, _ = exact64(x, k.transpose(0, 1)[:, None], v.transpose(0, 1)[:, None], seen.expand(kvh, group, n, n), scale)
+    check(out.view(n, kvh, group, d).permute(1, 2, 0, 3), o, tol)
+
+
 @pytest.mark.parametrize("base,step", [(20, 1), (29, 2 ** 10), (39, 2 ** 19), (39, 2 ** 20)])
 @pytest.mark.parametrize("n", [130, 3000])
 def test_trees(base, step, n):
