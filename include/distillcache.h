@@ -477,8 +477,8 @@ dc_status dc_paged_create(const dc_paged_config* cfg, dc_paged** out);
 dc_status dc_paged_destroy(dc_paged* h);
 
 /* Waits for the stream; DC_ERR_DEVICE if a kernel of this handle has reported an error since it was made: a page
- * number outside the pool, a position behind a table's end, starts out of order, a wait that ran out of time. Captures that are under way are
- * not disturbed; a stream that captures is refused. */
+ * number outside the pool, a position behind a table's end, starts out of order, a wait that ran out of time. (The report
+ * stays with the handle.) Captures that are under way are not disturbed; a stream that captures is refused. */
 dc_status dc_paged_check(dc_paged* h, void* stream);
 
 /* What dc_paged_append reads and writes; strides in elements, the innermost one is 1, every head starts on 16
@@ -520,7 +520,8 @@ dc_status dc_paged_append(dc_paged* h, const dc_paged_append_args* args, void* s
  * nothing). dc_paged_attend then reads a group's shared pages once, from the table row of its first sequence (which holds
  * them even where that sequence is not in use). Belongs
  * to the handle's device; waits for its own upload; may be made and freed while a stream captures, and must
- * outlive the graphs that hold its calls. */
+ * outlive the graphs that hold its calls. Made in 40 us; to be kept while its groups stay the same: destroy waits for all that
+ * the device has been given (3 us where that is nothing). */
 typedef struct dc_paged_shared dc_paged_shared;
 dc_status dc_paged_shared_create(dc_paged* h, const int* sizes, const int* tokens, int n, dc_paged_shared** out);
 dc_status dc_paged_shared_destroy(dc_paged_shared* g);
@@ -543,9 +544,10 @@ typedef struct {
 } dc_paged_attend_args;
 
 /* Softmax attention of one token of each sequence over its tokens in the cache; query head j uses KV head
- * j / (q_heads / kv_heads). Sums and statistics in 32 bits, the weights rounded to the cache's type for the
- * second product (in fp16 weights below 2^-38 of the largest are lost; of shared tokens n small ones are off by n 2^-30
- * of the largest at most), one rounding of the output, which must not overlap q or the cache. What the cache holds
+ * j / (q_heads / kv_heads). Sums and statistics in 32 bits. For the second product weights are rounded to the
+ * cache's type: for up to 8 query heads to a KV head to two numbers of it, of shared tokens and for more heads to one (in fp16
+ * weights below 2^-38 of the largest are lost; of shared tokens n small ones are off by n 2^-30 of the largest at most). One
+ * rounding of the output, which must not overlap q or the cache. What the cache holds
  * behind a sequence's last token leaves its output alone. A sequence that sees nothing has output 0 and lse
  * -infinity. tables' pages outside the pool count as not there, within a shared prefix as tokens of zeros
  * (dc_paged_check says so).
@@ -576,7 +578,8 @@ typedef struct {
  * a page's score is the largest over the KV head's query heads of sum_i max(q_i, 0) hi_i + min(q_i, 0) lo_i, with the
  * bounds of its keys. The products are exact in 32 bits (within their range) and of each two one is 0; their sum goes by
  * neighbouring pairs (dims 0 + 1, 2 + 3, ..., then those sums' pairs), each addition rounded to 32 bits, so that a selection does not depend on how
- * the work is divided. The first keep_first and the last keep_last pages of a sequence are always among them; then the
+ * the work is divided. (Infinity times the part of a query that is 0 is NaN: a page whose bounds are infinite has a score
+ * of infinity or NaN, and is looked at before others, as one that holds NaN is.) The first keep_first and the last keep_last pages of a sequence are always among them; then the
  * largest scores, the lower place where scores are equal, NaN before all numbers. out: places in the sequence's table
  * row, ascending, all pages where there are no more than count, -1 behind the last. A page number outside the pool: a
  * score of -infinity (dc_paged_check says so). */

@@ -24,10 +24,14 @@
 // boxes, each waits for the one before), and the last, then 1 us for a unit's end and 2.5 for the merge. (A CTA that
 // happened to have many short units came 10 us behind the others before the units' starts counted in the line: 90 us.)
 //
-// P is rounded to the cache's type because both operands of a product have one type: half a unit in the last place
-// of each weight, of the order of the result's own rounding; l sums the weights unrounded. In
-// fp16 the weights are up to 2^14 instead of 1, so that those above 2^-28 of the largest keep all their bits (taken back
-// where the warps' results are joined).
+// Both operands of a product have one type, so P enters the second one rounded to the cache's. For up to 8 rows it does in
+// two parts, the rounded weights and what the rounding left, rounded (16 bits of bf16 weights, 22 of fp16 ones): the results are
+// off by their own rounding alone (8 sequences of 16384 tokens against 64 bits, 8 KV heads of 128 dims, bf16: 1.64e-3, with one
+// part 2.15e-3), and HBM hides the second product (86.3 us, 86.0 with one part; 84.4 and 84.2 with 4 heads; the cases of
+// single tokens 0.1 to 0.2 us more). More rows do not hide it: 16 of them 53.0 us instead of 51.9 (64 dims: 37.6, 34.7), 32 68.0
+// instead of 58.4 (47.3, 42.4); their weights have one part, off by half a unit in the last place each, of the order of the result's
+// rounding. l sums the weights unrounded. In fp16 the weights are up to 2^14 instead of 1, so that those above 2^-28 of the
+// largest keep all their bits (taken back where the warps' results are joined).
 #include <algorithm>
 
 #include "dc_device.h"
@@ -89,6 +93,7 @@ template <int D, int NT>
 struct PagSmem {
   static constexpr int RB = 8 * NT;
   static constexpr int TEAMS = NT == 4 ? 1 : 2, WARPS = kPagTeam * TEAMS, THREADS = 32 * (WARPS + 2);
+  static constexpr bool TWO = NT == 1;          // P in two parts
   static constexpr int HALF = kPagTok * D * 2;  // a tile's K, or V
   static constexpr int STAGE = 2 * HALF;
   static constexpr int ST = D == 128 ? (NT == 4 ? 3 : 4) : (NT == 4 ? 6 : 8);  // (a stage belongs to one team)
@@ -452,7 +457,7 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
               }
             }
           }
-          uint32_t p[NT][2];
+          uint32_t p[NT][2], rest[NT][2];
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             // (the difference first: the rounding of m c alone is a factor of any size where scores are far from 0)
@@ -462,8 +467,14 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
             const float p2 = ex2(fmaf(z[t][2] - m0, c2, up2)), p3 = ex2(fmaf(z[t][3] - m1, c2, up2));
             l[t][0] += p0 + p2;
             l[t][1] += p1 + p3;
-            p[t][0] = transpose8(T::pack(p0, p1));
-            p[t][1] = transpose8(T::pack(p2, p3));
+            const uint32_t h0 = T::pack(p0, p1), h1 = T::pack(p2, p3);
+            p[t][0] = transpose8(h0);
+            p[t][1] = transpose8(h1);
+            if constexpr (L::TWO) {
+              const float2 f0 = T::two(h0), f1 = T::two(h1);
+              rest[t][0] = transpose8(T::pack(p0 - f0.x, p1 - f0.y));
+              rest[t][1] = transpose8(T::pack(p2 - f1.x, p3 - f1.y));
+            }
           }
 #pragma unroll
           for (int e = 0; e < D / 16; ++e) {
@@ -471,7 +482,10 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
             ldmatrix4_trans(f, chunk(base + v_at, vr, 2 * e + v_c));
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-              if (NT == 1 || t * 8 < nr) Frag<T>::mma(o[e][t], f, p[t][0], p[t][1]);
+              if (NT == 1 || t * 8 < nr) {
+                Frag<T>::mma(o[e][t], f, p[t][0], p[t][1]);
+                if constexpr (L::TWO) Frag<T>::mma(o[e][t], f, rest[t][0], rest[t][1]);
+              }
           }
         }
         __syncwarp();
