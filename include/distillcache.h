@@ -579,8 +579,9 @@ typedef struct {
  * bounds of its keys. The products are exact in 32 bits (within their range) and of each two one is 0; their sum goes by
  * neighbouring pairs (dims 0 + 1, 2 + 3, ..., then those sums' pairs), each addition rounded to 32 bits, so that a selection does not depend on how
  * the work is divided. (Infinity times the part of a query that is 0 is NaN: a page whose bounds are infinite has a score
- * of infinity or NaN, and is looked at before others, as one that holds NaN is.) The first keep_first and the last keep_last pages of a sequence are always among them; then the
- * largest scores, the lower place where scores are equal, NaN before all numbers. out: places in the sequence's table
+ * of infinity or NaN, and is looked at before others, as one that holds NaN is.) The first keep_first and the last
+ * keep_last pages of a sequence are always among them; then the largest scores, the lower place where scores are equal,
+ * NaN before all numbers. out: places in the sequence's table
  * row, ascending, all pages where there are no more than count, -1 behind the last. A page number outside the pool: a
  * score of -infinity (dc_paged_check says so). */
 dc_status dc_paged_select(dc_paged* h, const dc_paged_select_args* args, void* stream);
