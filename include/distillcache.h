@@ -546,7 +546,7 @@ typedef struct {
 /* Softmax attention of one token of each sequence over its tokens in the cache; query head j uses KV head
  * j / (q_heads / kv_heads). Sums and statistics in 32 bits. For the second product weights are rounded to the
  * cache's type: for up to 8 query heads to a KV head to two numbers of it, of shared tokens and for more heads to one (in fp16
- * weights below 2^-38 of the largest are lost; of shared tokens n small ones are off by n 2^-30 of the largest at most). One
+ * n small ones are off by n 2^-38 of the largest at most, those of shared tokens by n 2^-30). One
  * rounding of the output, which must not overlap q or the cache. What the cache holds
  * behind a sequence's last token leaves its output alone. A sequence that sees nothing has output 0 and lse
  * -infinity. tables' pages outside the pool count as not there, within a shared prefix as tokens of zeros

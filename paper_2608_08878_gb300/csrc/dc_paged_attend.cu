@@ -25,10 +25,10 @@
 // happened to have many short units came 10 us behind the others before the units' starts counted in the line: 90 us.)
 //
 // Both operands of a product have one type, so P enters the second one rounded to the cache's. For up to 8 rows it does in
-// two parts, the rounded weights and what the rounding left, rounded (16 bits of bf16 weights, 22 of fp16 ones): the results are
-// off by their own rounding alone (8 sequences of 16384 tokens against 64 bits, 8 KV heads of 128 dims, bf16: 1.64e-3, with one
-// part 2.15e-3), and HBM hides the second product (86.3 us, 86.0 with one part; 84.4 and 84.2 with 4 heads; the cases of
-// single tokens 0.1 to 0.2 us more). More rows do not hide it: 16 of them 53.0 us instead of 51.9 (64 dims: 37.6, 34.7), 32 68.0
+// two parts, the leading bits of each weight and the rest, rounded (16 bits of bf16 weights, 22 of fp16 ones): the results are off
+// by their own rounding alone (8 sequences of 16384 tokens against 64 bits, 8 KV heads of 128 dims, bf16: 1.64e-3, with one
+// part 2.15e-3), and HBM hides the second product (86.4 us, 86.1 with one part; 84.6 and 84.1 with 4 heads; single tokens of
+// few pages 0.1 to 0.2 us more). More rows do not hide it: 16 of them 53.0 us instead of 51.9 (64 dims: 37.6, 34.7), 32 68.0
 // instead of 58.4 (47.3, 42.4); their weights have one part, off by half a unit in the last place each, of the order of the result's
 // rounding. l sums the weights unrounded. In fp16 the weights are up to 2^14 instead of 1, so that those above 2^-28 of the
 // largest keep all their bits (taken back where the warps' results are joined).
@@ -54,6 +54,7 @@ struct Frag;
 template <>
 struct Frag<Bf16> {
   static constexpr float kRoom = 0.f;
+  using Type = TypeBf16;
   static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -63,6 +64,7 @@ struct Frag<Bf16> {
 template <>
 struct Frag<Half> {
   static constexpr float kRoom = 14.f;
+  using Type = TypeHalf;
   static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -467,13 +469,17 @@ __global__ void __launch_bounds__(PagSmem<D, NT>::THREADS, 1)
             const float p2 = ex2(fmaf(z[t][2] - m0, c2, up2)), p3 = ex2(fmaf(z[t][3] - m1, c2, up2));
             l[t][0] += p0 + p2;
             l[t][1] += p1 + p3;
-            const uint32_t h0 = T::pack(p0, p1), h1 = T::pack(p2, p3);
-            p[t][0] = transpose8(h0);
-            p[t][1] = transpose8(h1);
             if constexpr (L::TWO) {
-              const float2 f0 = T::two(h0), f1 = T::two(h1);
-              rest[t][0] = transpose8(T::pack(p0 - f0.x, p1 - f0.y));
-              rest[t][1] = transpose8(T::pack(p2 - f1.x, p3 - f1.y));
+              uint32_t h0, h1, r0, r1;
+              Frag<T>::Type::parts(p0, p1, h0, r0);
+              Frag<T>::Type::parts(p2, p3, h1, r1);
+              p[t][0] = transpose8(h0);
+              p[t][1] = transpose8(h1);
+              rest[t][0] = transpose8(r0);
+              rest[t][1] = transpose8(r1);
+            } else {
+              p[t][0] = transpose8(T::pack(p0, p1));
+              p[t][1] = transpose8(T::pack(p2, p3));
             }
           }
 #pragma unroll
