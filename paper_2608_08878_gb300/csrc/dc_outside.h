@@ -47,8 +47,10 @@ inline cudaError_t upload_now(void* dst, const void* src, size_t bytes) { return
 // stream in any case, of this one because it is not waited for (*captures; a captured kernel has not run).
 inline cudaError_t fetch_status(cudaStream_t s, const unsigned* status, unsigned (&words)[16], bool* captures) {
   cudaStreamCaptureStatus how = cudaStreamCaptureStatusNone;
-  if (cudaStreamIsCapturing(s, &how) != cudaSuccess) cudaGetLastError();
-  *captures = how != cudaStreamCaptureStatusNone;
+  const cudaError_t is = cudaStreamIsCapturing(s, &how);
+  if (is != cudaSuccess) cudaGetLastError();
+  // (the legacy stream would wait for a blocking stream that captures)
+  *captures = how != cudaStreamCaptureStatusNone || is == cudaErrorStreamCaptureImplicit;
   if (*captures) return cudaSuccess;
   const OutsideCapture outside;
   const cudaError_t e = cudaStreamSynchronize(s);
