@@ -19,8 +19,8 @@
 // tokens, 4 KV heads of 64 dims, 8 query heads each: 38.4 us with one team, 30.4 with two, 31.7 with four; of 128 dims 79.4
 // and 78.3 for the 130224 tokens below).
 //
-// What bounds it: HBM, behind some 9 us of latencies. 8 sequences of 32768 to 1 tokens, 8 KV heads of 128 dims: 524 MB in 78-80 us,
-// 6.6-6.7 TB/s; on the way to that 7.1 TB/s between the first tile, 4 us after the start (lengths, line, page number, first
+// What bounds it: HBM, behind some 9 us of latencies. 8 sequences of 32768 to 1 tokens, 8 KV heads of 128 dims: 524 MB in 79-80 us,
+// 6.5-6.6 TB/s; on the way to that 7.1 TB/s between the first tile, 4 us after the start (lengths, line, page number, first
 // boxes, each waits for the one before), and the last, then 1 us for a unit's end and 2.5 for the merge. (A CTA that
 // happened to have many short units came 10 us behind the others before the units' starts counted in the line: 90 us.)
 //

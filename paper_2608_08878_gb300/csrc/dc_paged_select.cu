@@ -350,8 +350,9 @@ template <class T, int D>
 cudaError_t launch_select(const SelectView& v, int num_sms, cudaStream_t s) {
   const long long rows = (long long)v.S * v.c.kvh;
   // CTAs of a row: one for 64 pages, as long as every one of them has an SM; above 8 of them 16 or 12, where the device holds
-  // that many clusters at once (us for 2048 pages of 64 and 4 query heads: 8 rows, clusters of 8, 12 and 16: 11.6, 10.8, 12.7,
-  // the last in two turns; 4 rows of 8 query heads: 14.2, 13.2, 10.9).
+  // that many clusters at once (us with 8 and with more, bounds in L2 and not: 8 rows of 2048 pages of 64 and 4 query heads, 12:
+  // 11.5, 10.9 and 14.5, 14.4; of 8192 30.0, 24.7 and 36.0, 30.2; 4 rows of 2048 and 8 query heads, 16: 14.5, 11.0 and 17.8, 14.1.
+  // 16 for 8 rows, in two turns: 12.7 instead of 10.9).
   int ctas = 1;
   while (v.W > v.count && ctas < 8 && ctas * 64 < v.W && rows * ctas * 2 <= num_sms) ctas *= 2;
   if (ctas == 8 && v.W > 8 * 64 && rows * 12 <= num_sms) {
