@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) page_select_kernel(const Selec
   grid_dep_launch();
   const int pages = a.pages_of(s);
   int* out = a.out + row * a.count;
-  const int* end = a.out + (long long)a.S * a.c.kvh * a.count;  // (debug builds: what every write is checked against)
+  [[maybe_unused]] const int* end = a.out + (long long)a.S * a.c.kvh * a.count;  // (debug builds: what every write is checked against)
   if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   if (pages <= a.count) {  // (the whole cluster)
     if (rank == 0)
